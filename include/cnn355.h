@@ -394,8 +394,74 @@ int cnn_deform_images(void* hip_stream, const float* d_src, size_t n_src, float*
                       const cnn_deform_params* p, uint64_t seed, uint64_t first_index,
                       const int32_t* d_src_index, float* d_displacement);
 
+/* ---- scores of classes --------------------------------------------------------------------------
+ * What a test pass is read with, and an error other than the library's own is trained on, from rows of sums x
+ * (before any soft-max) over classes.  With m = max_j x_j and S = log sum_j exp(x_j - m):
+ *   log p_j = (x_j - m) - S,   entropy H = - sum_j p_j log p_j
+ * A class with x_j = -inf is switched off: p_j = 0, log p_j = -inf, nothing in H.  A row with nothing left has
+ * log p = -inf everywhere, H = 0, m = S = -inf and a gradient of zero.  A row that holds +inf or NaN has no
+ * distribution: its numbers are NaN, its best classes -1.
+ *
+ *   cnn_class_scores: d_logits, device, rows of `classes` elements of `type`, row_stride elements apart.  Any of
+ *     the outputs may be NULL:
+ *     d_log_probs   [rows]           log p of the row's label d_labels[row]; 0 where that is outside [0, classes)
+ *                                    (a row without a label: padding)
+ *     d_entropy     [rows]           H
+ *     d_normaliser  [rows][2]        m and S, for cnn_class_scores_grad
+ *     d_top         [rows][n_top]    the n_top best classes, the best first, of equal ones the lower index first
+ *     d_top_log_probs [rows][n_top]  their log p
+ *     n_top <= 64 and <= classes.  d_labels may be NULL if d_log_probs is.  d_scratch: device memory, 256-byte
+ *     aligned, of at least cnn_class_scores_scratch_bytes (host-only; 0 where rows fill the chip: NULL will do),
+ *     free for other use once the stream has passed the call; calls that may overlap need one each.
+ *   cnn_class_scores_grad: d_grad, rows of `classes` elements of `type`, grad_stride apart, receives
+ *     g_l[row] d log p_label / dx + g_H[row] dH / dx, that is g_l ([j == label] - p_j) - g_H p_j (log p_j + H),
+ *     rounded once.  d_g_log_probs or d_g_entropy (NULL: zero) are [rows]; d_labels goes with the first, d_entropy
+ *     (from cnn_class_scores) with the second.  d_grad may be d_logits with the same stride; otherwise what lies
+ *     between the first and the last element of one must not overlap the other.  What lies between the rows is
+ *     left as it is.  (The error -log p_label averaged over n rows: g_l = -1/n.)
+ * Sums are fp32 for every type.  hip_stream: a hipStream_t (NULL: the default stream) of the current device.
+ * Asynchronous; nothing is allocated.  rows up to 2^31 - 1, classes up to 2^30; rows == 0 does nothing.
+ * Errors: CNN_E_ARG, CNN_E_SHAPE, CNN_E_WORKSPACE, CNN_E_HIP; the message is cnn_last_error(NULL)'s. */
+enum { CNN_TYPE_F32 = 0, CNN_TYPE_BF16 = 1, CNN_TYPE_F16 = 2 };
+int cnn_class_scores_scratch_bytes(size_t rows, size_t classes, int n_top, size_t* bytes);
+int cnn_class_scores(void* hip_stream, const void* d_logits, int type, size_t rows, size_t classes, size_t row_stride,
+                     const int32_t* d_labels, float* d_log_probs, float* d_entropy, float* d_normaliser,
+                     int n_top, int32_t* d_top, float* d_top_log_probs, void* d_scratch, size_t scratch_bytes);
+int cnn_class_scores_grad(void* hip_stream, const void* d_logits, int type, size_t rows, size_t classes, size_t row_stride,
+                          const int32_t* d_labels, const float* d_normaliser, const float* d_entropy,
+                          const float* d_g_log_probs, const float* d_g_entropy, void* d_grad, size_t grad_stride);
+
+/* ---- gradients of many tensors: their norm, clipping, the clipped update ---------------------------
+ * With N = sqrt(sum of the squares of all elements of all tensors) and f = max_norm / N where N > max_norm, else 1:
+ *   cnn_gradient_norm:  *d_norm = N
+ *   cnn_clip_gradients: out = f g, rounded once, of the gradients' types.  host_out == NULL: in place (not written
+ *                       at all where f is 1)
+ *   cnn_clipped_update: w <- w - lr f g for fp32 weights and gradients of any type (Sec. 3.4's adjustment)
+ * A norm that is infinite or NaN changes nothing: out = g, weights stay, and *d_norm (NULL where it is not wanted,
+ * but in cnn_gradient_norm) tells.  Squares, sums and products with f are double; the result depends on the list
+ * alone, bit for bit.
+ * host_grads, host_out, host_weights: host arrays of n tensors (read before the call returns) of device memory,
+ * elements contiguous, sizes and types (weights: CNN_TYPE_F32) of the same order; a size may be 0.  What is written
+ * must overlap nothing else in the call, but out[i] may be grads[i].  d_scratch: device memory, 256-byte aligned, at
+ * least cnn_gradient_scratch_bytes(n) (host-only), free once the stream has passed the call; calls that may
+ * overlap need one each.  max_norm >= 0 (inf: never clipped), lr finite.  Asynchronous; nothing is allocated.
+ * Errors: CNN_E_ARG, CNN_E_WORKSPACE, CNN_E_HIP; the message is cnn_last_error(NULL)'s. */
+typedef struct cnn_tensor {
+  void* d_data;
+  size_t n;    /* elements */
+  int type;    /* CNN_TYPE_* */
+} cnn_tensor;
+int cnn_gradient_scratch_bytes(size_t n, size_t* bytes);
+int cnn_gradient_norm(void* hip_stream, const cnn_tensor* host_grads, size_t n, float* d_norm, void* d_scratch,
+                      size_t scratch_bytes);
+int cnn_clip_gradients(void* hip_stream, const cnn_tensor* host_grads, const cnn_tensor* host_out, size_t n,
+                       float max_norm, float* d_norm, void* d_scratch, size_t scratch_bytes);
+int cnn_clipped_update(void* hip_stream, const cnn_tensor* host_weights, const cnn_tensor* host_grads, size_t n,
+                       float lr, float max_norm, float* d_norm, void* d_scratch, size_t scratch_bytes);
+
 /* Message for the last error on this handle (or, with net == NULL, of the last failed
- * cnn_create / cnn_workspace_bytes / cnn_arch_info / cnn_deform_images on this thread).  Never NULL. */
+ * cnn_create / cnn_workspace_bytes / cnn_arch_info / cnn_deform_images, or call without a handle, on this thread).
+ * Never NULL. */
 const char* cnn_last_error(const cnn_t* net);
 
 #ifdef __cplusplus

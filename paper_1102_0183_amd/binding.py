@@ -16,6 +16,7 @@ OK, E_SYNTAX, E_SHAPE, E_ARG, E_WORKSPACE, E_HIP, E_STATE = 0, -1, -2, -3, -4, -
 LAYER_INPUT, LAYER_CONV, LAYER_POOL, LAYER_FC = 0, 1, 2, 3
 MODE_STAGES, MODE_PERSISTENT, MODE_RESIDENT = 0, 1, 2
 OUTPUT_SOFTMAX_XENT, OUTPUT_TANH_SQERR = 0, 1
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
 
 _lib = None
 
@@ -85,6 +86,13 @@ def lib():
             "cnn_resident_spec_source": (C.c_int, [vp, vp, C.c_size_t]),
             "cnn_load_resident_code": (C.c_int, [vp, C.c_char_p]),
             "cnn_resident_code_active": (C.c_int, [vp]),
+            "cnn_class_scores_scratch_bytes": (C.c_int, [sz, sz, C.c_int, vp]),
+            "cnn_class_scores": (C.c_int, [vp, vp, C.c_int, sz, sz, sz, vp, vp, vp, vp, C.c_int, vp, vp, vp, sz]),
+            "cnn_class_scores_grad": (C.c_int, [vp, vp, C.c_int, sz, sz, sz, vp, vp, vp, vp, vp, vp, sz]),
+            "cnn_gradient_scratch_bytes": (C.c_int, [sz, vp]),
+            "cnn_gradient_norm": (C.c_int, [vp, vp, sz, vp, vp, sz]),
+            "cnn_clip_gradients": (C.c_int, [vp, vp, vp, sz, C.c_float, vp, vp, sz]),
+            "cnn_clipped_update": (C.c_int, [vp, vp, vp, sz, C.c_float, C.c_float, vp, vp, sz]),
             "cnn_last_error": (C.c_char_p, [vp]),
         }
         for name, (res, args) in sig.items():
@@ -106,7 +114,8 @@ EXPORTS = ["cnn_arch_info", "cnn_arch_info_xy", "cnn_workspace_bytes", "cnn_plan
            "cnn_set_matrix_cores", "cnn_set_launch_graph", "cnn_set_grid", "cnn_set_spin_limit", "cnn_set_barrier", "cnn_synchronize", "cnn_get_activation",
            "cnn_get_delta", "cnn_get_argmax", "cnn_get_loss", "cnn_debug_gradients", "cnn_get_stage_times", "cnn_measure_crossing", "cnn_measure_launch",
            "cnn_resident_spec_source", "cnn_load_resident_code", "cnn_resident_code_active", "cnn_debug_forward_batch_layer",
-           "cnn_deform_images", "cnn_last_error"]
+           "cnn_deform_images", "cnn_class_scores_scratch_bytes", "cnn_class_scores", "cnn_class_scores_grad",
+           "cnn_gradient_scratch_bytes", "cnn_gradient_norm", "cnn_clip_gradients", "cnn_clipped_update", "cnn_last_error"]
 
 
 def _err(handle=None):
@@ -142,6 +151,192 @@ def deform_images(d_src, d_dst, n, params, seed, first_index, d_src_index=None, 
                                  d_displacement.data_ptr() if d_displacement is not None else None)
     if rc:
         raise CnnError(rc, "cnn_deform_images", _err())
+
+
+def _element_type(t):
+    """TYPE_* of a tensor."""
+    import torch
+    kinds = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+    assert t.dtype in kinds, "expected float32, bfloat16 or float16"
+    return kinds[t.dtype]
+
+
+def _f32_of(t, shape, device):
+    """Address of a contiguous float32 tensor of this shape (None: None)."""
+    import torch
+    if t is None:
+        return None
+    assert t.device == device and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == shape, \
+        "expected a contiguous float32 tensor %r on %s" % (shape, device)
+    return t.data_ptr()
+
+
+def _labels_of(t, rows, device):
+    import torch
+    if t is None:
+        return None
+    assert t.device == device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == rows
+    return t.data_ptr()
+
+
+def _rows_of(t):
+    """(address, type, rows, classes, elements between rows) of a matrix whose rows are contiguous."""
+    assert t.is_cuda and t.dim() == 2, "expected a device matrix"
+    rows, classes = t.shape
+    assert classes <= 1 or t.stride(1) == 1, "the elements of a row must lie side by side"
+    return t.data_ptr(), _element_type(t), rows, classes, max(t.stride(0), classes) if rows <= 1 else t.stride(0)
+
+
+def _scratch_of(t, device):
+    import torch
+    if t is None or t.numel() == 0:
+        return None, 0
+    assert t.device == device and t.dtype == torch.uint8 and t.is_contiguous()
+    return t.data_ptr(), t.numel()
+
+
+class _On:
+    """The device of a call's tensors made the current one, and the stream it is issued on."""
+
+    def __init__(self, device, stream):
+        import torch
+        self._guard = torch.cuda.device(device)
+        self.stream = (stream or torch.cuda.current_stream(device)).cuda_stream
+
+    def __enter__(self):
+        self._guard.__enter__()
+        return self.stream
+
+    def __exit__(self, *e):
+        return self._guard.__exit__(*e)
+
+
+def class_scores_scratch_bytes(rows, classes, n_top=0):
+    """Host-only: bytes of scratch class_scores needs (0 where rows fill the chip)."""
+    n = C.c_size_t()
+    rc = lib().cnn_class_scores_scratch_bytes(int(rows), int(classes), int(n_top), C.addressof(n))
+    if rc:
+        raise CnnError(rc, "cnn_class_scores_scratch_bytes", _err())
+    return n.value
+
+
+def class_scores(d_logits, d_labels=None, d_log_probs=None, d_entropy=None, d_normaliser=None, d_top=None, d_top_log_probs=None,
+                 d_scratch=None, stream=None):
+    """cnn_class_scores: d_logits [rows][classes], float32, bfloat16 or float16, rows any stride apart; d_labels int32 [rows];
+    outputs (each of them or None) float32 d_log_probs [rows], d_entropy [rows], d_normaliser [rows][2], int32 d_top and
+    float32 d_top_log_probs [rows][n_top]; d_scratch: uint8, class_scores_scratch_bytes(rows, classes, n_top) of it.
+    Asynchronous on `stream` (a torch stream; None: the current)."""
+    import torch
+    x, kind, rows, classes, stride = _rows_of(d_logits)
+    dev = d_logits.device
+    n_top = 0
+    if d_top is not None:
+        n_top = d_top.shape[1]
+        assert d_top.device == dev and d_top.dtype == torch.int32 and d_top.is_contiguous() and tuple(d_top.shape) == (rows, n_top)
+    elif d_top_log_probs is not None:
+        n_top = d_top_log_probs.shape[1]
+    scratch, nbytes = _scratch_of(d_scratch, dev)
+    with _On(dev, stream) as s:
+        rc = lib().cnn_class_scores(s, x, kind, rows, classes, stride, _labels_of(d_labels, rows, dev), _f32_of(d_log_probs, (rows,), dev),
+                                    _f32_of(d_entropy, (rows,), dev), _f32_of(d_normaliser, (rows, 2), dev), n_top,
+                                    None if d_top is None else d_top.data_ptr(), _f32_of(d_top_log_probs, (rows, n_top), dev), scratch, nbytes)
+    if rc:
+        raise CnnError(rc, "cnn_class_scores", _err())
+
+
+def class_scores_grad(d_logits, d_grad, d_normaliser, d_labels=None, d_g_log_probs=None, d_entropy=None, d_g_entropy=None, stream=None):
+    """cnn_class_scores_grad: d_grad, of d_logits' shape and type (or d_logits itself), receives the gradient of
+    sum(d_g_log_probs * log_probs) + sum(d_g_entropy * entropy); d_normaliser and d_entropy as class_scores gave them."""
+    x, kind, rows, classes, stride = _rows_of(d_logits)
+    g, g_kind, g_rows, g_classes, g_stride = _rows_of(d_grad)
+    dev = d_logits.device
+    assert d_grad.device == dev and g_kind == kind and (g_rows, g_classes) == (rows, classes)
+    with _On(dev, stream) as s:
+        rc = lib().cnn_class_scores_grad(s, x, kind, rows, classes, stride, _labels_of(d_labels, rows, dev), _f32_of(d_normaliser, (rows, 2), dev),
+                                         _f32_of(d_entropy, (rows,), dev), _f32_of(d_g_log_probs, (rows,), dev),
+                                         _f32_of(d_g_entropy, (rows,), dev), g, g_stride)
+    if rc:
+        raise CnnError(rc, "cnn_class_scores_grad", _err())
+
+
+class Tensor(C.Structure):
+    """cnn_tensor of the header, field for field."""
+    _fields_ = [("d_data", C.c_void_p), ("n", C.c_size_t), ("type", C.c_int)]
+
+
+class TensorList:
+    """A list of device tensors of one device for the calls below, made once and used for every step: float32, bfloat16 or float16,
+    each dense (contiguous, or a permutation of it: the order of elements does not matter to a norm; lists that go together must
+    have the same one).  The tensors are kept."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.device = self.tensors[0].device if self.tensors else None
+        self.array = (Tensor * max(1, len(self.tensors)))()
+        self.orders = []
+        for k, t in enumerate(self.tensors):
+            assert t.is_cuda and t.device == self.device, "the tensors of a list lie on one device"
+            self.orders.append(_dense_order(t))
+            self.array[k] = Tensor(t.data_ptr(), t.numel(), _element_type(t))
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _dense_order(t):
+    """((size, stride) of the dimensions of more than one element) of a tensor without gaps; an error of any other."""
+    dims = [(n, s) for n, s in zip(t.shape, t.stride()) if n != 1]
+    at = 1
+    if t.numel():
+        for n, s in sorted(dims, key=lambda d: d[1]):
+            assert s == at, "expected a tensor without gaps"
+            at *= n
+    return () if t.is_contiguous() else tuple(dims)
+
+
+def gradient_scratch_bytes(n):
+    """Host-only: bytes of scratch the three calls below need for n tensors."""
+    b = C.c_size_t()
+    rc = lib().cnn_gradient_scratch_bytes(int(n), C.addressof(b))
+    if rc:
+        raise CnnError(rc, "cnn_gradient_scratch_bytes", _err())
+    return b.value
+
+
+def _over_gradients(grads, other, d_norm, d_scratch, stream, call):
+    import torch
+    dev = grads.device or (d_norm if d_norm is not None else d_scratch).device
+    if other is not None:
+        assert len(other) == len(grads) and (other.device == dev or not len(grads)) and other.orders == grads.orders, \
+            "lists that go together have the same tensors, laid out alike"
+    assert d_norm is None or (d_norm.device == dev and d_norm.dtype == torch.float32 and d_norm.numel() == 1)
+    scratch, nbytes = _scratch_of(d_scratch, dev)
+    with _On(dev, stream) as s:
+        rc = call(s, None if d_norm is None else d_norm.data_ptr(), scratch, nbytes)
+    if rc:
+        raise CnnError(rc, call.__name__, _err())
+
+
+def gradient_norm(grads, d_norm, d_scratch, stream=None):
+    """cnn_gradient_norm: d_norm (one float32) = the 2-norm over all elements of all tensors of a TensorList; d_scratch: uint8,
+    gradient_scratch_bytes(len(grads)) of it."""
+    def cnn_gradient_norm(s, norm, scratch, nbytes):
+        return lib().cnn_gradient_norm(s, grads.array, len(grads), norm, scratch, nbytes)
+    _over_gradients(grads, None, d_norm, d_scratch, stream, cnn_gradient_norm)
+
+
+def clip_gradients(grads, max_norm, d_scratch, out=None, d_norm=None, stream=None):
+    """cnn_clip_gradients: the gradients, in place or into the TensorList `out`, scaled to a norm of at most max_norm."""
+    def cnn_clip_gradients(s, norm, scratch, nbytes):
+        return lib().cnn_clip_gradients(s, grads.array, None if out is None else out.array, len(grads), float(max_norm), norm, scratch, nbytes)
+    _over_gradients(grads, out, d_norm, d_scratch, stream, cnn_clip_gradients)
+
+
+def clipped_update(weights, grads, lr, max_norm, d_scratch, d_norm=None, stream=None):
+    """cnn_clipped_update: weights (float32) -= lr * factor * grads, the factor that of clip_gradients."""
+    def cnn_clipped_update(s, norm, scratch, nbytes):
+        return lib().cnn_clipped_update(s, weights.array, grads.array, len(grads), float(lr), float(max_norm), norm, scratch, nbytes)
+    _over_gradients(grads, weights, d_norm, d_scratch, stream, cnn_clipped_update)
 
 
 def deform_on_matrix_cores(maps, rows, cols, sigma):

@@ -10,11 +10,13 @@
 #include <cstring>
 #include <memory>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
 #include "../../include/cnn355.h"
 #include "cnn355_dev.h"
+#include "cnn355_ops.h"
 #include "cnn355_flowspec.h"
 
 namespace cnn355 {
@@ -60,6 +62,13 @@ hipError_t launch_batch_outputs(hipStream_t stream, const float* sums, int n_sli
 hipError_t launch_batch_pack(hipStream_t stream, const BatchPackAll& all);
 hipError_t launch_deform(hipStream_t stream, const DeformJob& J);
 bool deform_mx_is_faster(const DeformJob& J);
+void score_parts(long long rows, int classes, int* parts, int* part_tiles);
+hipError_t launch_scores(hipStream_t stream, const ScoreJob& J);
+hipError_t launch_scores_grad(hipStream_t stream, const ScoreGradJob& J);
+hipError_t launch_squares(hipStream_t stream, const TensorJob& J, int workgroups, double* sums);
+hipError_t launch_norm(hipStream_t stream, const double* sums, int n, float* norm);
+hipError_t launch_scale(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, float* norm, int in_place);
+hipError_t launch_update(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, double lr, float* norm);
 }  // namespace cnn355
 
 using namespace cnn355;
@@ -1933,6 +1942,111 @@ int batch_plan(cnn* net, size_t batch, std::shared_ptr<const BatchKept>& out) {
 }
 }  // namespace
 
+// ---- many tensors ----------------------------------------------------------------------------------
+namespace {
+// What is wrong with a list (NULL: nothing).  to: what is written, or null; weights: to is fp32 whatever the gradients are.
+const char* check_list(const cnn_tensor* from, const cnn_tensor* to, size_t n, bool weights) {
+  if (n && !from) return "NULL list";
+  unsigned long long all = 0;
+  for (size_t i = 0; i < n; ++i) {
+    const cnn_tensor& g = from[i];
+    if (g.type != CNN_TYPE_F32 && g.type != CNN_TYPE_BF16 && g.type != CNN_TYPE_F16) return "unknown type";
+    if (g.n > (size_t)1 << 44 || (all += g.n) > (1ull << 44)) return "too many elements";
+    if (g.n && (!g.d_data || (uintptr_t)g.d_data % element_bytes(g.type))) return "a tensor is NULL or misaligned";
+    if (!to) continue;
+    if (to[i].n != g.n) return "sizes of the two lists differ";
+    if (to[i].type != (weights ? (int)CNN_TYPE_F32 : g.type)) return weights ? "weights must be fp32" : "types of the two lists differ";
+    if (g.n && (!to[i].d_data || (uintptr_t)to[i].d_data % element_bytes(to[i].type))) return "a tensor is NULL or misaligned";
+  }
+  if (!to) return nullptr;
+  // what is written overlaps nothing else: the written ranges in order, every other one looked up among them
+  struct Range { uintptr_t begin, end; };
+  std::vector<Range> out;
+  out.reserve(n);
+  auto range = [](const cnn_tensor& t) { return Range{(uintptr_t)t.d_data, (uintptr_t)t.d_data + t.n * element_bytes(t.type)}; };
+  for (size_t i = 0; i < n; ++i)
+    if (to[i].n) out.push_back(range(to[i]));
+  std::sort(out.begin(), out.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  for (size_t i = 1; i < out.size(); ++i)
+    if (out[i].begin < out[i - 1].end) return "tensors that are written overlap";
+  for (size_t i = 0; i < n; ++i) {
+    if (!from[i].n || (!weights && from[i].d_data == to[i].d_data)) continue;
+    const Range r = range(from[i]);
+    auto after = std::upper_bound(out.begin(), out.end(), r.begin, [](uintptr_t v, const Range& o) { return v < o.end; });   // the first that ends behind its start
+    if (after != out.end() && after->begin < r.end) return "a tensor that is written overlaps one that is read";
+  }
+  return nullptr;
+}
+
+// All tensors of a call, LIST_MOST to a launch: f(job, workgroups that leave sums).
+template <class F>
+hipError_t for_lists(const cnn_tensor* from, const cnn_tensor* to, size_t n, F f) {
+  auto chunks_of = [](size_t k) { return (k + LIST_CHUNK - 1) / LIST_CHUNK; };
+  unsigned long long all = 0;
+  for (size_t i = 0; i < n; ++i) all += chunks_of(from[i].n);
+  TensorJob J;
+  J.tensors = 0; J.chunks = 0; J.first_sum = 0; J.sums = 0;
+  bool any = false;
+  auto flush = [&]() {
+    const int w = (int)std::max<unsigned long long>(1, std::min<unsigned long long>(J.chunks, all ? (LIST_SUMS * (unsigned long long)J.chunks + all - 1) / all : 1));
+    hipError_t e = f(J, w);
+    J.first_sum += w;
+    J.tensors = 0; J.chunks = 0;
+    any = true;
+    return e;
+  };
+  for (size_t i = 0; i < n; ++i) {
+    if (!from[i].n) continue;
+    const int t = J.tensors++;
+    J.from[t] = (const CNN_GLOBAL void*)from[i].d_data;
+    J.to[t] = (CNN_GLOBAL void*)(to ? to[i].d_data : nullptr);
+    J.n[t] = from[i].n; J.type[t] = (unsigned char)from[i].type; J.chunk[t] = J.chunks;
+    J.chunks += (unsigned)chunks_of(from[i].n);
+    if (J.tensors < LIST_MOST) continue;
+    hipError_t e = flush();
+    if (e != hipSuccess) return e;
+  }
+  return J.tensors || !any ? flush() : hipSuccess;
+}
+
+// apply 0: the norm only, 1: scale, 2: update
+int over_gradients(const char* call, hipStream_t stream, const cnn_tensor* grads, const cnn_tensor* out, size_t n, int apply,
+                          float max_norm, float lr, float* d_norm, void* d_scratch, size_t scratch_bytes) {
+  if (n > (size_t)1 << 24) return fail(nullptr, CNN_E_ARG, std::string(call) + ": too many tensors");
+  const char* why = nullptr;
+  try {
+    why = check_list(grads, out, n, apply == 2);
+  } catch (const std::bad_alloc&) {
+    why = "no host memory for so many tensors";
+  }
+  if (why) return fail(nullptr, CNN_E_ARG, std::string(call) + ": " + why);
+  size_t need = 0;
+  cnn_gradient_scratch_bytes(n, &need);
+  if (!d_scratch || ((uintptr_t)d_scratch & 255u) || scratch_bytes < need)
+    return fail(nullptr, CNN_E_WORKSPACE, std::string(call) + ": scratch must be 256-byte aligned device memory of at least " + std::to_string(need) + " bytes");
+  double* sums = (double*)d_scratch;
+  int n_sums = 0;
+  hipError_t e = for_lists(grads, nullptr, n, [&](const TensorJob& J, int w) {
+    n_sums = J.first_sum + w;
+    return launch_squares(stream, J, w, sums);
+  });
+  if (e == hipSuccess && apply == 0) e = launch_norm(stream, sums, n_sums, d_norm);
+  if (e == hipSuccess && apply != 0) {
+    e = for_lists(grads, out, n, [&](TensorJob& J, int) {
+      J.sums = n_sums;
+      float* norm = d_norm;
+      d_norm = nullptr;   // (the first launch gives it)
+      bool in_place = true;
+      for (int t = 0; t < J.tensors; ++t) in_place = in_place && J.from[t] == (const CNN_GLOBAL void*)J.to[t];
+      return apply == 1 ? launch_scale(stream, J, sums, max_norm, norm, in_place) : launch_update(stream, J, sums, max_norm, lr, norm);
+    });
+  }
+  if (e != hipSuccess) return fail(nullptr, CNN_E_HIP, std::string(call) + ": " + hipGetErrorString(e));
+  return CNN_OK;
+}
+
+}  // namespace
+
 extern "C" {
 
 int cnn_arch_info(const char* arch, int32_t* n_layers, int32_t* info, int32_t max_layers) {
@@ -2711,6 +2825,110 @@ int cnn_deform_images(void* hip_stream, const float* d_src, size_t n_src, float*
   hipError_t e = launch_deform((hipStream_t)hip_stream, J);
   if (e != hipSuccess) return fail(nullptr, CNN_E_HIP, std::string("cnn_deform_images: ") + hipGetErrorString(e));
   return CNN_OK;
+}
+
+// ---- scores of classes ----------------------------------------------------------------------------
+static int check_rows(const char* call, int type, size_t rows, size_t classes, size_t stride) {
+  if (type != CNN_TYPE_F32 && type != CNN_TYPE_BF16 && type != CNN_TYPE_F16) return fail(nullptr, CNN_E_ARG, std::string(call) + ": unknown type");
+  if (classes < 1 || classes > (size_t)1 << 30 || rows > 0x7fffffffull)
+    return fail(nullptr, CNN_E_SHAPE, std::string(call) + ": 1 to 2^30 classes, at most 2^31 - 1 rows");
+  if (stride < classes || stride > ((size_t)1 << 60) / (rows ? rows : 1))
+    return fail(nullptr, CNN_E_ARG, std::string(call) + ": rows of fewer elements than classes, or too far apart");
+  return CNN_OK;
+}
+
+static size_t score_scratch(size_t rows, size_t classes, int n_top, int* parts, int* part_tiles) {
+  score_parts((long long)rows, (int)classes, parts, part_tiles);
+  return *parts == 1 ? 0 : rows * *parts * (16 + 8 * (size_t)n_top);
+}
+
+int cnn_class_scores_scratch_bytes(size_t rows, size_t classes, int n_top, size_t* bytes) {
+  if (!bytes) return fail(nullptr, CNN_E_ARG, "cnn_class_scores_scratch_bytes: NULL argument");
+  int rc = check_rows("cnn_class_scores_scratch_bytes", CNN_TYPE_F32, rows, classes, classes);
+  if (rc) return rc;
+  if (n_top < 0 || n_top > SCORE_TOP || (size_t)n_top > classes)
+    return fail(nullptr, CNN_E_ARG, "cnn_class_scores_scratch_bytes: 0 to 64 best classes, no more than there are");
+  int parts, part_tiles;
+  *bytes = rows ? score_scratch(rows, classes, n_top, &parts, &part_tiles) : 0;
+  return CNN_OK;
+}
+
+int cnn_class_scores(void* hip_stream, const void* d_logits, int type, size_t rows, size_t classes, size_t row_stride,
+                     const int32_t* d_labels, float* d_log_probs, float* d_entropy, float* d_normaliser,
+                     int n_top, int32_t* d_top, float* d_top_log_probs, void* d_scratch, size_t scratch_bytes) {
+  int rc = check_rows("cnn_class_scores", type, rows, classes, row_stride);
+  if (rc) return rc;
+  if (n_top < 0 || n_top > SCORE_TOP || (size_t)n_top > classes)
+    return fail(nullptr, CNN_E_ARG, "cnn_class_scores: 0 to 64 best classes, no more than there are");
+  if (rows == 0) return CNN_OK;
+  if (!d_logits || (uintptr_t)d_logits % element_bytes(type)) return fail(nullptr, CNN_E_ARG, "cnn_class_scores: d_logits is NULL or misaligned");
+  if (d_log_probs && !d_labels) return fail(nullptr, CNN_E_ARG, "cnn_class_scores: log probabilities of labels without labels");
+  if (!d_top && !d_top_log_probs) n_top = 0;
+  ScoreJob J;
+  J.x = (const CNN_GLOBAL void*)d_logits; J.labels = d_labels; J.log_probs = d_log_probs; J.entropy = d_entropy; J.normaliser = d_normaliser;
+  J.top = n_top ? d_top : nullptr; J.top_log_probs = n_top ? d_top_log_probs : nullptr;
+  J.rows = (long long)rows; J.stride = (long long)row_stride; J.classes = (int)classes; J.type = type; J.n_top = n_top;
+  const size_t need = score_scratch(rows, classes, n_top, &J.parts, &J.part_tiles);
+  if (need && (!d_scratch || ((uintptr_t)d_scratch & 255u) || scratch_bytes < need))
+    return fail(nullptr, CNN_E_WORKSPACE, "cnn_class_scores: scratch must be 256-byte aligned device memory of at least " + std::to_string(need) + " bytes");
+  J.part_sums = need ? (float*)d_scratch : nullptr;
+  J.part_best = need ? (unsigned long long*)((char*)d_scratch + rows * J.parts * 16) : nullptr;
+  hipError_t e = launch_scores((hipStream_t)hip_stream, J);
+  if (e != hipSuccess) return fail(nullptr, CNN_E_HIP, std::string("cnn_class_scores: ") + hipGetErrorString(e));
+  return CNN_OK;
+}
+
+int cnn_class_scores_grad(void* hip_stream, const void* d_logits, int type, size_t rows, size_t classes, size_t row_stride,
+                          const int32_t* d_labels, const float* d_normaliser, const float* d_entropy,
+                          const float* d_g_log_probs, const float* d_g_entropy, void* d_grad, size_t grad_stride) {
+  int rc = check_rows("cnn_class_scores_grad", type, rows, classes, row_stride);
+  if (!rc) rc = check_rows("cnn_class_scores_grad", type, rows, classes, grad_stride);
+  if (rc) return rc;
+  if (rows == 0) return CNN_OK;
+  const size_t size = element_bytes(type);
+  if (!d_logits || !d_grad || !d_normaliser || (uintptr_t)d_logits % size || (uintptr_t)d_grad % size)
+    return fail(nullptr, CNN_E_ARG, "cnn_class_scores_grad: NULL or misaligned argument");
+  if (!d_g_log_probs && !d_g_entropy) return fail(nullptr, CNN_E_ARG, "cnn_class_scores_grad: neither of the two has a gradient");
+  if ((d_g_log_probs && !d_labels) || (d_g_entropy && !d_entropy))
+    return fail(nullptr, CNN_E_ARG, "cnn_class_scores_grad: a gradient of log probabilities without labels, or of the entropy without the entropy");
+  const uintptr_t x0 = (uintptr_t)d_logits, x1 = x0 + ((rows - 1) * row_stride + classes) * size;
+  const uintptr_t g0 = (uintptr_t)d_grad, g1 = g0 + ((rows - 1) * grad_stride + classes) * size;
+  if (x0 < g1 && g0 < x1 && !(x0 == g0 && (row_stride == grad_stride || rows == 1)))
+    return fail(nullptr, CNN_E_ARG, "cnn_class_scores_grad: d_grad overlaps d_logits");
+  ScoreGradJob J;
+  J.x = (const CNN_GLOBAL void*)d_logits; J.grad = (CNN_GLOBAL void*)d_grad; J.labels = d_labels; J.normaliser = d_normaliser; J.entropy = d_entropy;
+  J.g_log_probs = d_g_log_probs; J.g_entropy = d_g_entropy;
+  J.rows = (long long)rows; J.stride = (long long)row_stride; J.grad_stride = (long long)grad_stride; J.classes = (int)classes; J.type = type;
+  hipError_t e = launch_scores_grad((hipStream_t)hip_stream, J);
+  if (e != hipSuccess) return fail(nullptr, CNN_E_HIP, std::string("cnn_class_scores_grad: ") + hipGetErrorString(e));
+  return CNN_OK;
+}
+
+// ---- many tensors ----------------------------------------------------------------------------------
+int cnn_gradient_scratch_bytes(size_t n, size_t* bytes) {
+  if (!bytes) return fail(nullptr, CNN_E_ARG, "cnn_gradient_scratch_bytes: NULL argument");
+  if (n > (size_t)1 << 24) return fail(nullptr, CNN_E_ARG, "cnn_gradient_scratch_bytes: too many tensors");
+  *bytes = (LIST_SUMS + n / LIST_MOST + 2) * sizeof(double);
+  return CNN_OK;
+}
+
+int cnn_gradient_norm(void* hip_stream, const cnn_tensor* host_grads, size_t n, float* d_norm, void* d_scratch, size_t scratch_bytes) {
+  if (!d_norm) return fail(nullptr, CNN_E_ARG, "cnn_gradient_norm: NULL argument");
+  return over_gradients("cnn_gradient_norm", (hipStream_t)hip_stream, host_grads, nullptr, n, 0, 0.f, 0.f, d_norm, d_scratch, scratch_bytes);
+}
+
+int cnn_clip_gradients(void* hip_stream, const cnn_tensor* host_grads, const cnn_tensor* host_out, size_t n, float max_norm, float* d_norm,
+                       void* d_scratch, size_t scratch_bytes) {
+  if (!(max_norm >= 0.f)) return fail(nullptr, CNN_E_ARG, "cnn_clip_gradients: max_norm is negative or NaN");
+  return over_gradients("cnn_clip_gradients", (hipStream_t)hip_stream, host_grads, host_out ? host_out : host_grads, n, 1, max_norm, 0.f, d_norm,
+                        d_scratch, scratch_bytes);
+}
+
+int cnn_clipped_update(void* hip_stream, const cnn_tensor* host_weights, const cnn_tensor* host_grads, size_t n, float lr, float max_norm,
+                       float* d_norm, void* d_scratch, size_t scratch_bytes) {
+  if (!(max_norm >= 0.f) || !std::isfinite(lr)) return fail(nullptr, CNN_E_ARG, "cnn_clipped_update: max_norm is negative or NaN, or lr not finite");
+  if (n && !host_weights) return fail(nullptr, CNN_E_ARG, "cnn_clipped_update: NULL list");
+  return over_gradients("cnn_clipped_update", (hipStream_t)hip_stream, host_grads, host_weights, n, 2, max_norm, lr, d_norm, d_scratch, scratch_bytes);
 }
 
 // development aid, host only: 1 where the smoothing of such a call runs on the matrix cores, 0 where as sums over a line

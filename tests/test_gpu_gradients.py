@@ -1,0 +1,196 @@
+"""The norm of gradients over many tensors, clipping by it and the clipped update, against 64-bit sums, through the C ABI.
+Needs a GPU.
+
+Tolerances.  Squares and sums are doubles: the norm is off by half a step of fp32 (2^-24) and nothing that shows beside it.  A
+clipped gradient is a product in double, rounded to fp32 and from there to its type: half a step of the type, 2^-24 more of the
+value where that is not fp32; half of its smallest value below the normal ones.  An updated weight is rounded once."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_1102_0183_amd import binding
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def _tensors(counts, kinds, seed, scale=1e-2, gap=0):
+    """Tensors one behind the other in a buffer of each type, gap elements between them."""
+    import torch
+    gen = torch.Generator(device="cuda:0").manual_seed(seed)
+    out = []
+    need = {k: sum(c + gap for c, q in zip(counts, kinds) if q == k) for k in set(kinds)}
+    flats = {k: torch.full((n + 1,), 7.0, dtype=getattr(torch, k), device="cuda:0") for k, n in need.items()}
+    at = dict.fromkeys(need, 0)
+    for c, k in zip(counts, kinds):
+        t = flats[k][at[k]:at[k] + c]
+        t.copy_(torch.randn(c, generator=gen, device="cuda:0") * scale)
+        out.append(t)
+        at[k] += c + gap
+    return out, flats
+
+
+def _norm(tensors):
+    return math.sqrt(math.fsum(float(t.double().dot(t.double())) for t in tensors))
+
+
+def _scratch(n):
+    import torch
+    return torch.empty(binding.gradient_scratch_bytes(n), dtype=torch.uint8, device="cuda:0")
+
+
+def _run_norm(tensors, stream=None):
+    import torch
+    got = torch.full((1,), 5.0, device="cuda:0")
+    binding.gradient_norm(binding.TensorList(tensors), got, _scratch(len(tensors)), stream)
+    return got
+
+
+def _check_clip(before, after, norm, limit):
+    import torch
+    f = float(np.float32(limit)) / norm if norm > limit else 1.0   # (the limit is a float)
+    for b, a in zip(before, after):
+        if f == 1.0:
+            assert torch.equal(a, b)
+            continue
+        fi = torch.finfo(b.dtype)
+        want = b.double() * f
+        tol = want.abs() * (fi.eps / 2 * (1 + 1e-6) + (0 if b.dtype == torch.float32 else U)) + fi.smallest_normal * fi.eps / 2 * (1 + 1e-6)
+        assert ((a.double() - want).abs() <= tol).all()
+
+
+LISTS = [
+    [1], [2, 0, 3], [0], [], [7], [4095, 1], [8192], [8193, 8191], [20, 320, 40, 20000, 150, 54000, 10, 1500], [1 << 20, 3, 5, 100003],
+    [33] * 127, [33] * 128, [65, 1] * 65, [5] * 256 + [9000] * 2, [0] * 130 + [17], [3] * 600,
+]
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "float16", "mixed"])
+@pytest.mark.parametrize("counts", LISTS, ids=lambda c: "%dx%d" % (len(c), sum(c)))
+def test_norm_clip_and_update(counts, kind):
+    import torch
+    kinds = [kind if kind != "mixed" else ("float32", "bfloat16", "float16")[k % 3] for k in range(len(counts))]
+    grads, flats = _tensors(counts, kinds, 3, gap=1)
+    before = [g.clone() for g in grads]
+    norm = _norm(grads)
+    got = _run_norm(grads)
+    assert abs(float(got) - norm) <= norm * U * (1 + 1e-6)
+    assert torch.equal(got, _run_norm(grads))
+    for limit in (0.37 * norm, 2 * norm + 1, math.inf, 0.0):
+        # into other tensors
+        out = [torch.full_like(g, 3.0) for g in grads]
+        n = torch.zeros(1, device="cuda:0")
+        binding.clip_gradients(binding.TensorList(grads), limit, _scratch(len(counts)), out=binding.TensorList(out), d_norm=n)
+        assert torch.equal(n, got)
+        _check_clip(before, out, norm, limit)
+        assert all(torch.equal(b, g) for b, g in zip(before, grads))
+        # in place
+        binding.clip_gradients(binding.TensorList(grads), limit, _scratch(len(counts)))
+        assert all(torch.equal(o, g) for o, g in zip(out, grads))
+        for g, b in zip(grads, before):
+            g.copy_(b)
+        # the update
+        weights, w_flats = _tensors(counts, ["float32"] * len(counts), 4, scale=0.05, gap=3)
+        w0 = [w.clone() for w in weights]
+        binding.clipped_update(binding.TensorList(weights), binding.TensorList(grads), 0.1, limit, _scratch(len(counts)), d_norm=n)
+        assert torch.equal(n, got)
+        step = float(np.float32(0.1)) * (float(np.float32(limit)) / norm if norm > limit else 1.0)   # (lr and the limit are floats)
+        for a, b, g in zip(weights, w0, grads):
+            want = b.double() - step * g.double()
+            assert ((a.double() - want).abs() <= want.abs() * U + step * g.double().abs() * U * 1e-3).all()
+        assert all((f[_gaps(counts, kinds, k, 1)] == 7).all() for k, f in flats.items())
+        assert all((f[_gaps(counts, ["float32"] * len(counts), "float32", 3)] == 7).all() for f in w_flats.values())
+
+
+def _gaps(counts, kinds, kind, gap):
+    """Where the buffer of a type has its gaps."""
+    at, out = 0, []
+    for c, k in zip(counts, kinds):
+        if k == kind:
+            out += range(at + c, at + c + gap)
+            at += c + gap
+    return out
+
+
+def test_values_whose_squares_no_float_holds():
+    import torch
+    big = torch.full((1000,), 3e38, device="cuda:0")
+    small = torch.full((1000,), 1e-42, device="cuda:0")
+    assert float(_run_norm([small])) == pytest.approx(float(small[0].double()) * math.sqrt(1000), rel=1e-3)
+    norm = _run_norm([big])
+    assert math.isinf(float(norm))               # no float holds it, a double does:
+    out = [torch.empty_like(big)]
+    binding.clip_gradients(binding.TensorList([big]), 1.0, _scratch(1), out=binding.TensorList(out))
+    _check_clip([big], out, _norm([big]), 1.0)
+    t = [torch.tensor([1e30, 1.0], device="cuda:0"), torch.tensor([1e-30], device="cuda:0")]
+    assert abs(float(_run_norm(t)) - 1e30) <= 1e30 * 2 * U
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("where", [0, 5000, 30000])
+def test_a_norm_that_is_no_number_changes_nothing(bad, where):
+    import torch
+    for kind in ("float32", "bfloat16", "float16"):
+        grads, _ = _tensors([20000, 10001], [kind, kind], 8)
+        (grads[0] if where < 20000 else grads[1])[where % 20000] = bad
+        before = [g.clone() for g in grads]
+        same = lambda a, b: torch.equal(a.isnan(), b.isnan()) and torch.equal(a[~a.isnan()], b[~b.isnan()])  # noqa: E731
+        out = [torch.zeros_like(g) for g in grads]
+        n = torch.zeros(1, device="cuda:0")
+        binding.clip_gradients(binding.TensorList(grads), 1e-3, _scratch(2), out=binding.TensorList(out), d_norm=n)
+        assert (math.isnan(float(n)) if math.isnan(bad) else float(n) == math.inf)
+        assert all(same(o, b) for o, b in zip(out, before))
+        binding.clip_gradients(binding.TensorList(grads), 1e-3, _scratch(2))
+        assert all(same(g, b) for g, b in zip(grads, before))
+        weights = [torch.ones(20000, device="cuda:0"), torch.ones(10001, device="cuda:0")]
+        binding.clipped_update(binding.TensorList(weights), binding.TensorList(grads), 0.1, 1.0, _scratch(2))
+        assert all((w == 1).all() for w in weights)
+
+
+def test_tensors_that_are_dense_in_another_order():
+    import torch
+    g = [torch.randn(5, 7, 11, device="cuda:0").permute(2, 0, 1), torch.randn(64, 33, device="cuda:0").t()]
+    assert abs(float(_run_norm(g)) - _norm([t.contiguous().view(-1) for t in g])) <= 100 * 2 * U
+    out = [torch.empty_like(t) for t in g]       # (laid out alike)
+    binding.clip_gradients(binding.TensorList(g), 1.0, _scratch(2), out=binding.TensorList(out))
+    _check_clip(g, out, _norm([t.contiguous().view(-1) for t in g]), 1.0)
+    with pytest.raises(AssertionError):
+        binding.clip_gradients(binding.TensorList(g), 1.0, _scratch(2), out=binding.TensorList([t.contiguous() for t in g]))
+    for bad in (torch.empty(4, 6, device="cuda:0")[:, ::2], torch.empty(4, 6, device="cuda:0")[:, :5], torch.empty(1, 6, device="cuda:0").expand(4, 6),
+                torch.empty(6, device="cuda:0").double(), torch.empty(6)):
+        with pytest.raises(AssertionError):
+            binding.TensorList([bad])
+
+
+def test_streams_and_a_captured_step():
+    import torch
+    counts = [20, 320, 40, 20000, 150, 54000, 10, 1500] * 20          # two launches of tensors
+    grads, flats = _tensors(counts, ["bfloat16"] * len(counts), 11)
+    weights, w_flats = _tensors(counts, ["float32"] * len(counts), 12)
+    gl, wl, scratch = binding.TensorList(grads), binding.TensorList(weights), _scratch(len(counts))
+    want = _run_norm(grads)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(s1):
+            a = _run_norm(grads, s1)
+        with torch.cuda.stream(s2):
+            b = _run_norm(grads, s2)
+        torch.cuda.synchronize()
+        assert torch.equal(a, want) and torch.equal(b, want)
+    norm = torch.zeros(1, device="cuda:0")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.clipped_update(wl, gl, 0.01, 0.5, scratch, d_norm=norm)
+    f, w = flats["bfloat16"], w_flats["float32"]
+    for seed in (1, 2, 3):
+        f[:-1].copy_(torch.randn(f.numel() - 1, generator=torch.Generator(device="cuda:0").manual_seed(seed), device="cuda:0") * seed)
+        keep = w.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed, n = w.clone(), norm.clone()
+        w.copy_(keep)
+        binding.clipped_update(wl, gl, 0.01, 0.5, scratch, d_norm=norm)
+        torch.cuda.synchronize()
+        assert torch.equal(w, replayed) and torch.equal(norm, n) and not torch.equal(w, keep)
