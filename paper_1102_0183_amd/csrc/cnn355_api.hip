@@ -65,7 +65,8 @@ bool deform_mx_is_faster(const DeformJob& J);
 void score_parts(long long rows, int classes, int* parts, int* part_tiles);
 hipError_t launch_scores(hipStream_t stream, const ScoreJob& J);
 hipError_t launch_scores_grad(hipStream_t stream, const ScoreGradJob& J);
-hipError_t launch_squares(hipStream_t stream, const TensorJob& J, int workgroups, double* sums);
+hipError_t launch_table(hipStream_t stream, const TensorJob& J, TensorEntry* at);
+hipError_t launch_squares(hipStream_t stream, const TensorJob& J, double* sums);
 hipError_t launch_norm(hipStream_t stream, const double* sums, int n, float* norm);
 hipError_t launch_scale(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, float* norm, int in_place);
 hipError_t launch_update(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, double lr, float* norm);
@@ -1978,40 +1979,9 @@ const char* check_list(const cnn_tensor* from, const cnn_tensor* to, size_t n, b
   return nullptr;
 }
 
-// All tensors of a call, LIST_MOST to a launch: f(job, workgroups that leave sums).
-template <class F>
-hipError_t for_lists(const cnn_tensor* from, const cnn_tensor* to, size_t n, F f) {
-  auto chunks_of = [](size_t k) { return (k + LIST_CHUNK - 1) / LIST_CHUNK; };
-  unsigned long long all = 0;
-  for (size_t i = 0; i < n; ++i) all += chunks_of(from[i].n);
-  TensorJob J;
-  J.tensors = 0; J.chunks = 0; J.first_sum = 0; J.sums = 0;
-  bool any = false;
-  auto flush = [&]() {
-    const int w = (int)std::max<unsigned long long>(1, std::min<unsigned long long>(J.chunks, all ? (LIST_SUMS * (unsigned long long)J.chunks + all - 1) / all : 1));
-    hipError_t e = f(J, w);
-    J.first_sum += w;
-    J.tensors = 0; J.chunks = 0;
-    any = true;
-    return e;
-  };
-  for (size_t i = 0; i < n; ++i) {
-    if (!from[i].n) continue;
-    const int t = J.tensors++;
-    J.from[t] = (const CNN_GLOBAL void*)from[i].d_data;
-    J.to[t] = (CNN_GLOBAL void*)(to ? to[i].d_data : nullptr);
-    J.n[t] = from[i].n; J.type[t] = (unsigned char)from[i].type; J.chunk[t] = J.chunks;
-    J.chunks += (unsigned)chunks_of(from[i].n);
-    if (J.tensors < LIST_MOST) continue;
-    hipError_t e = flush();
-    if (e != hipSuccess) return e;
-  }
-  return J.tensors || !any ? flush() : hipSuccess;
-}
-
 // apply 0: the norm only, 1: scale, 2: update
 int over_gradients(const char* call, hipStream_t stream, const cnn_tensor* grads, const cnn_tensor* out, size_t n, int apply,
-                          float max_norm, float lr, float* d_norm, void* d_scratch, size_t scratch_bytes) {
+                   float max_norm, float lr, float* d_norm, void* d_scratch, size_t scratch_bytes) {
   if (n > (size_t)1 << 24) return fail(nullptr, CNN_E_ARG, std::string(call) + ": too many tensors");
   const char* why = nullptr;
   try {
@@ -2025,22 +1995,37 @@ int over_gradients(const char* call, hipStream_t stream, const cnn_tensor* grads
   if (!d_scratch || ((uintptr_t)d_scratch & 255u) || scratch_bytes < need)
     return fail(nullptr, CNN_E_WORKSPACE, std::string(call) + ": scratch must be 256-byte aligned device memory of at least " + std::to_string(need) + " bytes");
   double* sums = (double*)d_scratch;
-  int n_sums = 0;
-  hipError_t e = for_lists(grads, nullptr, n, [&](const TensorJob& J, int w) {
-    n_sums = J.first_sum + w;
-    return launch_squares(stream, J, w, sums);
-  });
-  if (e == hipSuccess && apply == 0) e = launch_norm(stream, sums, n_sums, d_norm);
-  if (e == hipSuccess && apply != 0) {
-    e = for_lists(grads, out, n, [&](TensorJob& J, int) {
-      J.sums = n_sums;
-      float* norm = d_norm;
-      d_norm = nullptr;   // (the first launch gives it)
-      bool in_place = true;
-      for (int t = 0; t < J.tensors; ++t) in_place = in_place && J.from[t] == (const CNN_GLOBAL void*)J.to[t];
-      return apply == 1 ? launch_scale(stream, J, sums, max_norm, norm, in_place) : launch_update(stream, J, sums, max_norm, lr, norm);
-    });
+  TensorEntry* table = (TensorEntry*)(sums + LIST_SUMS);
+  size_t live = 0;
+  for (size_t i = 0; i < n; ++i) live += grads[i].n != 0;
+  // the tensors that hold something, in the kernels' argument where they fit there, else in memory, an argument after the other
+  TensorJob J;
+  J.table = nullptr; J.tensors = 0; J.chunks = 0; J.sums = 0;
+  hipError_t e = hipSuccess;
+  bool in_place = true;
+  size_t written = 0;
+  auto flush = [&]() {
+    if (live <= LIST_MOST || !J.tensors || e != hipSuccess) return;
+    e = launch_table(stream, J, table + written);
+    written += J.tensors;
+    J.tensors = 0;
+  };
+  for (size_t i = 0; i < n; ++i) {
+    if (!grads[i].n) continue;
+    if (J.tensors == LIST_MOST) flush();
+    TensorEntry& t = J.e[J.tensors++];
+    t.from = (const CNN_GLOBAL void*)grads[i].d_data; t.to = (CNN_GLOBAL void*)(out ? out[i].d_data : nullptr);
+    t.n = grads[i].n; t.type = grads[i].type; t.chunk = J.chunks;
+    J.chunks += (unsigned)((grads[i].n * element_bytes(grads[i].type) + LIST_CHUNK - 1) / LIST_CHUNK);
+    in_place = in_place && t.from == (const CNN_GLOBAL void*)t.to;
   }
+  flush();
+  if (live > LIST_MOST) { J.table = (const CNN_GLOBAL TensorEntry*)table; J.tensors = (int)live; }
+  J.sums = (int)std::max(1u, std::min(J.chunks, (unsigned)LIST_SUMS));
+  if (e == hipSuccess) e = launch_squares(stream, J, sums);
+  if (e == hipSuccess && apply == 0) e = launch_norm(stream, sums, J.sums, d_norm);
+  if (e == hipSuccess && apply == 1) e = launch_scale(stream, J, sums, max_norm, d_norm, in_place);
+  if (e == hipSuccess && apply == 2) e = launch_update(stream, J, sums, max_norm, lr, d_norm);
   if (e != hipSuccess) return fail(nullptr, CNN_E_HIP, std::string(call) + ": " + hipGetErrorString(e));
   return CNN_OK;
 }
@@ -2908,7 +2893,7 @@ int cnn_class_scores_grad(void* hip_stream, const void* d_logits, int type, size
 int cnn_gradient_scratch_bytes(size_t n, size_t* bytes) {
   if (!bytes) return fail(nullptr, CNN_E_ARG, "cnn_gradient_scratch_bytes: NULL argument");
   if (n > (size_t)1 << 24) return fail(nullptr, CNN_E_ARG, "cnn_gradient_scratch_bytes: too many tensors");
-  *bytes = (LIST_SUMS + n / LIST_MOST + 2) * sizeof(double);
+  *bytes = LIST_SUMS * sizeof(double) + (n > LIST_MOST ? n * sizeof(TensorEntry) : 0);
   return CNN_OK;
 }
 

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #define CNN_GLOBAL __attribute__((address_space(1)))
 #include "cnn355_ops.h"
@@ -21,6 +22,8 @@ namespace {
 
 constexpr int GT = 256;   // threads of a workgroup
 
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+typedef unsigned v2u_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -36,59 +39,128 @@ __device__ __forceinline__ double sum_of_workgroup(double s, double* lds) {
   return s;
 }
 
-// the tensor that chunk c is of
-__device__ __forceinline__ int tensor_of(const TensorJob& J, unsigned c) {
-  int lo = 0, hi = J.tensors;   // chunk[lo] <= c < chunk[hi]
-  while (hi - lo > 1) {
+// ---- chunks ----
+constexpr int NV = LIST_CHUNK / GT / 16;   // loads of 16 bytes a lane
+
+struct Piece {   // a chunk of a tensor
+  const CNN_GLOBAL char* from;
+  CNN_GLOBAL void* to;             // the tensor's beginning,
+  unsigned long long begin;        // its first element in it
+  int n, type;                     // elements (0: no chunk)
+};
+
+// Chunk c's piece.  t: the tensor of a chunk that was looked up before (DOWN: of one behind c, else of one in front), then this one's.
+template <bool FAR, bool DOWN>
+__device__ __forceinline__ Piece piece_of(const TensorJob& J, unsigned i, int& t) {
+  Piece p = {nullptr, nullptr, 0, 0, 0};
+  if (i >= J.chunks) return p;
+  const unsigned c = DOWN ? J.chunks - 1 - i : i;
+  auto first = [&](int k) { return FAR ? J.table[k].chunk : J.e[k].chunk; };
+  int lo = DOWN ? 0 : t, hi = DOWN ? t + 1 : J.tensors;
+  while (hi - lo > 1) {   // first(lo) <= c, and c < first(hi) where there is one
     const int mid = (lo + hi) >> 1;
-    if (J.chunk[mid] <= c) lo = mid; else hi = mid;
+    if (first(mid) <= c) lo = mid; else hi = mid;
   }
-  return lo;
+  t = lo;
+  unsigned long long n;
+  if (FAR) {
+    const CNN_GLOBAL TensorEntry* e = J.table + t;
+    p.from = (const CNN_GLOBAL char*)e->from; p.to = e->to; p.type = e->type; n = e->n;
+  } else {
+    const TensorEntry& e = J.e[t];
+    p.from = (const CNN_GLOBAL char*)e.from; p.to = e.to; p.type = e.type; n = e.n;
+  }
+  const unsigned long long at = (unsigned long long)(c - first(t)) * LIST_CHUNK;
+  const int shift = p.type == ELEMENT_F32 ? 2 : 1;
+  p.from += at;
+  p.begin = at >> shift;
+  p.n = (int)min(n - p.begin, (unsigned long long)(LIST_CHUNK >> shift));
+  return p;
+}
+__device__ __forceinline__ bool whole(const Piece& p) { return p.n << (p.type == ELEMENT_F32 ? 2 : 1) == LIST_CHUNK; }
+
+// A workgroup's chunks, every gridDim.x-th of all, so that what is read side by side lies side by side (DOWN: from the last one
+// on): full(piece, its elements, 16 bytes a lane and load) or part(piece).  The next one is looked up while the loads of a chunk
+// are under way.  FOURS: types of 16 bits in loads of 8 bytes, two in the place of one of 16, so that the fp32 values that belong
+// to a wavefront's load lie side by side too.
+template <bool FAR, bool DOWN, bool FOURS, class Full, class Part>
+__device__ __forceinline__ void for_chunks(const TensorJob& J, Full full, Part part) {
+  int t = DOWN ? J.tensors - 1 : 0;
+  Piece p = piece_of<FAR, DOWN>(J, blockIdx.x, t);
+  for (unsigned i = blockIdx.x; i < J.chunks; i += gridDim.x) {
+    Piece next;
+    if (whole(p)) {
+      v4u r[NV];
+      if (FOURS && p.type != ELEMENT_F32) {
+#pragma unroll
+        for (int q = 0; q < 2 * NV; ++q) {
+          const v2u v = *(const CNN_GLOBAL v2u_any*)(p.from + (q * GT + threadIdx.x) * 8);
+          r[q >> 1][(q & 1) * 2] = v[0];
+          r[q >> 1][(q & 1) * 2 + 1] = v[1];
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < NV; ++q) r[q] = *(const CNN_GLOBAL v4u_any*)(p.from + (q * GT + threadIdx.x) * 16);
+      }
+      next = piece_of<FAR, DOWN>(J, i + gridDim.x, t);
+      full(p, r);
+    } else {
+      next = piece_of<FAR, DOWN>(J, i + gridDim.x, t);
+      part(p);
+    }
+    p = next;
+  }
+}
+
+// f(a constant of the type)
+template <class F>
+__device__ __forceinline__ void by_type(int type, F f) {
+  switch (type) {
+    case ELEMENT_F32: f(std::integral_constant<int, ELEMENT_F32>()); break;
+    case ELEMENT_BF16: f(std::integral_constant<int, ELEMENT_BF16>()); break;
+    default: f(std::integral_constant<int, ELEMENT_F16>()); break;
+  }
 }
 
 // ---- the sum of squares ----
-template <int TYPE>
-__device__ __forceinline__ double squares(const CNN_GLOBAL void* from, unsigned long long begin, unsigned long long n) {
-  typedef Element<TYPE> E;
-  typedef typename E::T T;
-  constexpr int V = E::V, N = LIST_CHUNK / GT / V;
-  const CNN_GLOBAL T* g = (const CNN_GLOBAL T*)from + begin;
-  double s = 0.0;
-  if (n - begin >= LIST_CHUNK) {
-    v4u r[N];
-#pragma unroll
-    for (int q = 0; q < N; ++q) r[q] = *(const CNN_GLOBAL v4u_any*)(g + (q * GT + threadIdx.x) * V);
-#pragma unroll
-    for (int q = 0; q < N; ++q)
-#pragma unroll
-      for (int j = 0; j < V; ++j) { const double v = E::get(r[q], j); s = fma(v, v, s); }
-    return s;
-  }
-  const int left = (int)(n - begin), whole = left / V;
-  for (int i = threadIdx.x; i < whole; i += GT) {
-    const v4u r = *(const CNN_GLOBAL v4u_any*)(g + i * V);
-#pragma unroll
-    for (int j = 0; j < V; ++j) { const double v = E::get(r, j); s = fma(v, v, s); }
-  }
-  const int last = whole * V + (int)threadIdx.x;
-  if (last < left) { const double v = E::get(g[last]); s = fma(v, v, s); }
-  return s;
-}
-
+template <bool FAR>
 __global__ void __launch_bounds__(GT) k_squares(TensorJob J, CNN_GLOBAL double* sums) {
   __shared__ double lds[GT / 64];
   double s = 0.0;
-  for (unsigned c = blockIdx.x; c < J.chunks; c += gridDim.x) {
-    const int t = tensor_of(J, c);
-    const unsigned long long begin = (unsigned long long)(c - J.chunk[t]) * LIST_CHUNK;
-    switch (J.type[t]) {
-      case ELEMENT_F32: s += squares<ELEMENT_F32>(J.from[t], begin, J.n[t]); break;
-      case ELEMENT_BF16: s += squares<ELEMENT_BF16>(J.from[t], begin, J.n[t]); break;
-      default: s += squares<ELEMENT_F16>(J.from[t], begin, J.n[t]); break;
-    }
-  }
+  for_chunks<FAR, false, false>(
+      J,
+      [&](const Piece& p, const v4u (&r)[NV]) {
+        by_type(p.type, [&](auto type) {
+          typedef Element<decltype(type)::value> E;
+#pragma unroll
+          for (int q = 0; q < NV; ++q)
+#pragma unroll
+            for (int j = 0; j < E::V; ++j) { const double v = E::get(r[q], j); s = fma(v, v, s); }
+        });
+      },
+      [&](const Piece& p) {
+        by_type(p.type, [&](auto type) {
+          typedef Element<decltype(type)::value> E;
+          const CNN_GLOBAL typename E::T* g = (const CNN_GLOBAL typename E::T*)p.from;
+          const int n = p.n / E::V, last = n * E::V + (int)threadIdx.x;
+          for (int i = threadIdx.x; i < n; i += GT) {
+            const v4u r = *(const CNN_GLOBAL v4u_any*)(g + i * E::V);
+#pragma unroll
+            for (int j = 0; j < E::V; ++j) { const double v = E::get(r, j); s = fma(v, v, s); }
+          }
+          if (last < p.n) { const double v = E::get(g[last]); s = fma(v, v, s); }
+        });
+      });
   s = sum_of_workgroup(s, lds);
-  if (threadIdx.x == 0) sums[J.first_sum + blockIdx.x] = s;
+  if (threadIdx.x == 0) sums[blockIdx.x] = s;
+}
+
+// entries that fit no kernel's argument, to memory
+__global__ void __launch_bounds__(128) k_table(TensorJob J, CNN_GLOBAL TensorEntry* at) {
+  if ((int)threadIdx.x >= J.tensors) return;
+  const TensorEntry& e = J.e[threadIdx.x];
+  CNN_GLOBAL TensorEntry* o = at + threadIdx.x;
+  o->from = e.from; o->to = e.to; o->n = e.n; o->chunk = e.chunk; o->type = e.type;
 }
 
 __device__ __forceinline__ double norm_of(const CNN_GLOBAL double* sums, int n, double* lds) {
@@ -104,122 +176,136 @@ __global__ void __launch_bounds__(GT) k_norm(const CNN_GLOBAL double* sums, int 
 }
 
 // ---- what is done with it ----
+// A gradient times the factor, to its type.  fp32: the product in double.  Types of 16 bits: in float, the factor as the sum of
+// two of them times a power of two, which keeps its 48 bits whatever its size (conversions to double and back bound fp16:
+// 145 us for 100 M elements, bf16 108).
+struct Factor {
+  double f;
+  float high, low;   // f = (high + low) 2^e, 0.5 <= high + low < 1
+  int e;
+};
+__device__ __forceinline__ Factor factor_of(double f) {
+  Factor r;
+  r.f = f;
+  const double m = frexp(f, &r.e);
+  r.high = (float)m;
+  r.low = (float)(m - r.high);
+  return r;
+}
 template <int TYPE>
-__device__ __forceinline__ void scale(const CNN_GLOBAL void* from, CNN_GLOBAL void* to, unsigned long long begin, unsigned long long n, double f) {
-  typedef Element<TYPE> E;
-  typedef typename E::T T;
-  constexpr int V = E::V, N = LIST_CHUNK / GT / V;
-  const CNN_GLOBAL T* g = (const CNN_GLOBAL T*)from + begin;
-  CNN_GLOBAL T* o = (CNN_GLOBAL T*)to + begin;
-  auto one = [&](float v) { return E::make((float)(v * f)); };
-  auto sixteen = [&](v4u r) {
-    union { v4u v; T e[V]; } out;
-#pragma unroll
-    for (int j = 0; j < V; ++j) out.e[j] = one(E::get(r, j));
-    return out.v;
-  };
-  if (n - begin >= LIST_CHUNK) {
-    v4u r[N];
-#pragma unroll
-    for (int q = 0; q < N; ++q) r[q] = *(const CNN_GLOBAL v4u_any*)(g + (q * GT + threadIdx.x) * V);
-#pragma unroll
-    for (int q = 0; q < N; ++q) *(CNN_GLOBAL v4u_any*)(o + (q * GT + threadIdx.x) * V) = sixteen(r[q]);
-    return;
-  }
-  const int left = (int)(n - begin), whole = left / V;
-  for (int i = threadIdx.x; i < whole; i += GT) *(CNN_GLOBAL v4u_any*)(o + i * V) = sixteen(*(const CNN_GLOBAL v4u_any*)(g + i * V));
-  const int last = whole * V + (int)threadIdx.x;
-  if (last < left) o[last] = one(E::get(g[last]));
+__device__ __forceinline__ typename Element<TYPE>::T times(float g, const Factor& f) {
+  if (TYPE == ELEMENT_F32) return Element<TYPE>::make((float)(g * f.f));
+  return Element<TYPE>::make(ldexpf(fmaf(g, f.high, g * f.low), f.e));
 }
 
 template <int TYPE>
-__device__ __forceinline__ void update(const CNN_GLOBAL void* from, CNN_GLOBAL void* to, unsigned long long begin, unsigned long long n, double f) {
+__device__ __forceinline__ v4u times(v4u r, const Factor& f) {
   typedef Element<TYPE> E;
-  typedef typename E::T T;
-  constexpr int V = E::V, N = LIST_CHUNK / GT / V, W = V / 4;
-  const CNN_GLOBAL T* g = (const CNN_GLOBAL T*)from + begin;
-  CNN_GLOBAL float* w = (CNN_GLOBAL float*)to + begin;
-  auto one = [&](float w, float g) { return (float)fma(-f, (double)g, (double)w); };
-  auto some = [&](int at, v4u r, const v4f (&v)[W]) {
+  v4u v;
 #pragma unroll
-    for (int k = 0; k < W; ++k) {
-      v4f o;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = one(v[k][j], E::get(r, 4 * k + j));
-      *(CNN_GLOBAL v4f_any*)(w + at + 4 * k) = o;
-    }
-  };
-  const int left = n - begin < LIST_CHUNK ? (int)(n - begin) : LIST_CHUNK, whole = left / V;
-  if (left == LIST_CHUNK) {
-    constexpr int B = N < 4 ? N : 4;   // (loads that wait together)
-#pragma unroll 1
-    for (int q0 = 0; q0 < N; q0 += B) {
-      v4u r[B];
-      v4f v[B][W];
-#pragma unroll
-      for (int q = 0; q < B; ++q) {
-        const int at = ((q0 + q) * GT + threadIdx.x) * V;
-        r[q] = *(const CNN_GLOBAL v4u_any*)(g + at);
-#pragma unroll
-        for (int k = 0; k < W; ++k) v[q][k] = *(const CNN_GLOBAL v4f_any*)(w + at + 4 * k);
-      }
-#pragma unroll
-      for (int q = 0; q < B; ++q) some(((q0 + q) * GT + threadIdx.x) * V, r[q], v[q]);
-    }
-    return;
-  }
-  for (int i = threadIdx.x; i < whole; i += GT) {
-    const v4u r = *(const CNN_GLOBAL v4u_any*)(g + i * V);
-    v4f v[W];
-#pragma unroll
-    for (int k = 0; k < W; ++k) v[k] = *(const CNN_GLOBAL v4f_any*)(w + i * V + 4 * k);
-    some(i * V, r, v);
-  }
-  const int last = whole * V + (int)threadIdx.x;
-  if (last < left) w[last] = one(w[last], E::get(g[last]));
+  for (int j = 0; j < E::V; ++j) E::put(v, j, times<TYPE>(E::get(r, j), f));
+  return v;
 }
 
-// UPDATE: to holds weights (float), `lr` is the rate; else to holds the clipped gradients, which may be `from` themselves.
-template <bool UPDATE>
-__global__ void __launch_bounds__(GT) k_apply(TensorJob J, const CNN_GLOBAL double* sums, double max_norm, double lr, CNN_GLOBAL float* norm, int in_place) {
+// to = f g; to may be the gradients themselves
+template <bool FAR>
+__global__ void __launch_bounds__(GT) k_scale(TensorJob J, const CNN_GLOBAL double* sums, double max_norm, CNN_GLOBAL float* norm, int in_place) {
   __shared__ double lds[GT / 64];
   const double v = norm_of(sums, J.sums, lds);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
-  const bool finite = v < __builtin_inf();
-  double f = finite && v > max_norm ? max_norm / v : 1.0;
-  if (UPDATE) {
-    if (!finite) return;
-    f *= lr;
-  } else if (in_place && f == 1.0) {
-    return;
-  }
-  // the last chunks first: they are the ones that the first launch read last, and may still be in the cache
-  for (unsigned k = blockIdx.x; k < J.chunks; k += gridDim.x) {
-    const unsigned c = J.chunks - 1 - k;
-    const int t = tensor_of(J, c);
-    const unsigned long long begin = (unsigned long long)(c - J.chunk[t]) * LIST_CHUNK;
-    if (UPDATE) {
-      switch (J.type[t]) {
-        case ELEMENT_F32: update<ELEMENT_F32>(J.from[t], J.to[t], begin, J.n[t], f); break;
-        case ELEMENT_BF16: update<ELEMENT_BF16>(J.from[t], J.to[t], begin, J.n[t], f); break;
-        default: update<ELEMENT_F16>(J.from[t], J.to[t], begin, J.n[t], f); break;
-      }
-    } else {
-      switch (J.type[t]) {
-        case ELEMENT_F32: scale<ELEMENT_F32>(J.from[t], J.to[t], begin, J.n[t], f); break;
-        case ELEMENT_BF16: scale<ELEMENT_BF16>(J.from[t], J.to[t], begin, J.n[t], f); break;
-        default: scale<ELEMENT_F16>(J.from[t], J.to[t], begin, J.n[t], f); break;
-      }
-    }
-  }
+  const bool clips = v < __builtin_inf() && v > max_norm;
+  if (!clips && in_place) return;
+  const Factor f = factor_of(clips ? max_norm / v : 1.0);
+  // the last chunks first: they are the ones that the launch before read last, and may still be in a cache
+  for_chunks<FAR, true, false>(
+      J,
+      [&](const Piece& p, const v4u (&r)[NV]) {
+        by_type(p.type, [&](auto type) {
+          constexpr int TYPE = decltype(type)::value;
+          CNN_GLOBAL typename Element<TYPE>::T* o = (CNN_GLOBAL typename Element<TYPE>::T*)p.to + p.begin;
+#pragma unroll
+          for (int q = 0; q < NV; ++q)
+            __builtin_nontemporal_store(clips ? times<TYPE>(r[q], f) : r[q], (CNN_GLOBAL v4u_any*)(o + (q * GT + threadIdx.x) * Element<TYPE>::V));
+        });
+      },
+      [&](const Piece& p) {
+        by_type(p.type, [&](auto type) {
+          constexpr int TYPE = decltype(type)::value, V = Element<TYPE>::V;
+          typedef typename Element<TYPE>::T T;
+          const CNN_GLOBAL T* g = (const CNN_GLOBAL T*)p.from;
+          CNN_GLOBAL T* o = (CNN_GLOBAL T*)p.to + p.begin;
+          const int n = p.n / V, last = n * V + (int)threadIdx.x;
+          for (int i = threadIdx.x; i < n; i += GT) {
+            const v4u r = *(const CNN_GLOBAL v4u_any*)(g + i * V);
+            *(CNN_GLOBAL v4u_any*)(o + i * V) = clips ? times<TYPE>(r, f) : r;
+          }
+          if (last < p.n) o[last] = clips ? times<TYPE>(Element<TYPE>::get(g[last]), f) : g[last];
+        });
+      });
+}
+
+// to (weights) -= f lr g
+template <bool FAR>
+__global__ void __launch_bounds__(GT) k_update(TensorJob J, const CNN_GLOBAL double* sums, double max_norm, double lr, CNN_GLOBAL float* norm) {
+  __shared__ double lds[GT / 64];
+  const double v = norm_of(sums, J.sums, lds);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+  if (!(v < __builtin_inf())) return;
+  const double f = -lr * (v > max_norm ? max_norm / v : 1.0);
+  auto one = [&](float w, float g) { return (float)fma(f, (double)g, (double)w); };
+  for_chunks<FAR, true, true>(
+      J,
+      [&](const Piece& p, const v4u (&r)[NV]) {
+        by_type(p.type, [&](auto type) {
+          typedef Element<decltype(type)::value> E;
+          CNN_GLOBAL float* w = (CNN_GLOBAL float*)p.to + p.begin;
+          if constexpr (E::V == 4) {
+            v4f o[NV];
+#pragma unroll
+            for (int q = 0; q < NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + threadIdx.x) * 4));
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) o[q][j] = one(o[q][j], E::get(r[q], j));
+              __builtin_nontemporal_store(o[q], (CNN_GLOBAL v4f_any*)(w + (q * GT + threadIdx.x) * 4));
+            }
+          } else {
+            v4f o[2 * NV];
+#pragma unroll
+            for (int q = 0; q < 2 * NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + threadIdx.x) * 4));
+#pragma unroll
+            for (int q = 0; q < 2 * NV; ++q) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) o[q][j] = one(o[q][j], E::get(r[q >> 1], (q & 1) * 4 + j));
+              __builtin_nontemporal_store(o[q], (CNN_GLOBAL v4f_any*)(w + (q * GT + threadIdx.x) * 4));
+            }
+          }
+        });
+      },
+      [&](const Piece& p) {
+        by_type(p.type, [&](auto type) {
+          typedef Element<decltype(type)::value> E;
+          const CNN_GLOBAL typename E::T* g = (const CNN_GLOBAL typename E::T*)p.from;
+          CNN_GLOBAL float* w = (CNN_GLOBAL float*)p.to + p.begin;
+          for (int i = threadIdx.x; i < p.n; i += GT) w[i] = one(w[i], E::get(g[i]));
+        });
+      });
 }
 
 constexpr unsigned APPLY_GRID = 2048;
 
+unsigned apply_grid(const TensorJob& J) { return std::max(1u, std::min(J.chunks, APPLY_GRID)); }
+
 }  // namespace
 
-hipError_t launch_squares(hipStream_t stream, const TensorJob& J, int workgroups, double* sums) {
-  hipLaunchKernelGGL(k_squares, dim3((unsigned)workgroups), dim3(GT), 0, stream, J, (CNN_GLOBAL double*)sums);
+hipError_t launch_table(hipStream_t stream, const TensorJob& J, TensorEntry* at) {
+  hipLaunchKernelGGL(k_table, dim3(1), dim3(128), 0, stream, J, (CNN_GLOBAL TensorEntry*)at);
+  return hipGetLastError();
+}
+
+hipError_t launch_squares(hipStream_t stream, const TensorJob& J, double* sums) {
+  if (J.table) hipLaunchKernelGGL(k_squares<true>, dim3((unsigned)J.sums), dim3(GT), 0, stream, J, (CNN_GLOBAL double*)sums);
+  else hipLaunchKernelGGL(k_squares<false>, dim3((unsigned)J.sums), dim3(GT), 0, stream, J, (CNN_GLOBAL double*)sums);
   return hipGetLastError();
 }
 
@@ -229,14 +315,16 @@ hipError_t launch_norm(hipStream_t stream, const double* sums, int n, float* nor
 }
 
 hipError_t launch_scale(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, float* norm, int in_place) {
-  hipLaunchKernelGGL(k_apply<false>, dim3(std::max(1u, std::min(J.chunks, APPLY_GRID))), dim3(GT), 0, stream, J, (const CNN_GLOBAL double*)sums, max_norm, 0.0,
-                     (CNN_GLOBAL float*)norm, in_place);
+  const CNN_GLOBAL double* s = (const CNN_GLOBAL double*)sums;
+  if (J.table) hipLaunchKernelGGL(k_scale<true>, dim3(apply_grid(J)), dim3(GT), 0, stream, J, s, max_norm, (CNN_GLOBAL float*)norm, in_place);
+  else hipLaunchKernelGGL(k_scale<false>, dim3(apply_grid(J)), dim3(GT), 0, stream, J, s, max_norm, (CNN_GLOBAL float*)norm, in_place);
   return hipGetLastError();
 }
 
 hipError_t launch_update(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, double lr, float* norm) {
-  hipLaunchKernelGGL(k_apply<true>, dim3(std::max(1u, std::min(J.chunks, APPLY_GRID))), dim3(GT), 0, stream, J, (const CNN_GLOBAL double*)sums, max_norm, lr,
-                     (CNN_GLOBAL float*)norm, 0);
+  const CNN_GLOBAL double* s = (const CNN_GLOBAL double*)sums;
+  if (J.table) hipLaunchKernelGGL(k_update<true>, dim3(apply_grid(J)), dim3(GT), 0, stream, J, s, max_norm, lr, (CNN_GLOBAL float*)norm);
+  else hipLaunchKernelGGL(k_update<false>, dim3(apply_grid(J)), dim3(GT), 0, stream, J, s, max_norm, lr, (CNN_GLOBAL float*)norm);
   return hipGetLastError();
 }
 

@@ -46,19 +46,23 @@ struct ScoreGradJob {
 };
 
 // ---- many tensors -------------------------------------------------------------------------------
-constexpr int LIST_MOST = 128;     // tensors of one launch: the descriptor travels as a kernel argument (below 4 KB)
-constexpr int LIST_CHUNK = 8192;   // elements that a workgroup takes at a time
-constexpr int LIST_SUMS = 1024;    // workgroups of a call that leave a sum, at most, and one a launch more
+constexpr int LIST_MOST = 120;     // tensors of a kernel's argument (below 4 KB)
+constexpr int LIST_CHUNK = 16384;  // bytes: gradients are cut into chunks of so many
+constexpr int LIST_SUMS = 1024;    // workgroups that leave a sum, at most
 
+struct TensorEntry {
+  const CNN_GLOBAL void* from;     // gradients
+  CNN_GLOBAL void* to;             // what is written: clipped gradients, or weights (float)
+  unsigned long long n;            // elements, at least one
+  unsigned int chunk;              // its first chunk among those of all tensors
+  int type;
+};
 struct TensorJob {
-  const CNN_GLOBAL void* from[LIST_MOST];   // gradients
-  CNN_GLOBAL void* to[LIST_MOST];           // what is written: clipped gradients, or weights (float)
-  unsigned long long n[LIST_MOST];          // elements
-  unsigned int chunk[LIST_MOST];            // first chunk of every tensor
-  unsigned char type[LIST_MOST];
+  const CNN_GLOBAL TensorEntry* table;   // where they do not fit in `e`
   int tensors;
-  unsigned int chunks;                      // of all
-  int first_sum, sums;                      // of this launch's workgroups; of all of them (where they are read)
+  unsigned int chunks;             // of all tensors
+  int sums;                        // workgroups that leave a sum
+  TensorEntry e[LIST_MOST];
 };
 
 }  // namespace cnn355
