@@ -48,15 +48,15 @@ template <> struct Element<ELEMENT_F16> : Element16 {
   static __device__ __forceinline__ void put(v4u& r, int j, T v) { put_bits(r, j, __builtin_bit_cast(unsigned short, v)); }
 };
 
-// 16 bytes from element `at` on of a row, -inf from element `end` on
+// 16 bytes from element `at` on of a row, -inf from element `end` on and in front of `begin`
 template <int TYPE>
-__device__ __forceinline__ v4u load16(const CNN_GLOBAL typename Element<TYPE>::T* row, int at, int end) {
+__device__ __forceinline__ v4u load16(const CNN_GLOBAL typename Element<TYPE>::T* row, int at, int end, int begin = 0) {
   typedef Element<TYPE> E;
-  if (at + E::V <= end) return *(const CNN_GLOBAL v4u_any*)(row + at);
+  if (at >= begin && at + E::V <= end) return *(const CNN_GLOBAL v4u_any*)(row + at);
   v4u r = {E::MASKED, E::MASKED, E::MASKED, E::MASKED};
 #pragma unroll
   for (int j = 0; j < E::V; ++j)
-    if (at + j < end) E::put(r, j, row[at + j]);
+    if (at + j >= begin && at + j < end) E::put(r, j, row[at + j]);
   return r;
 }
 

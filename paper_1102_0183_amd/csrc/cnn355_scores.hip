@@ -9,12 +9,12 @@
 // wavefronts and workgroups that share a row join their three numbers in the same way.  All of it is held in 32 bits.
 //
 // The best classes ride along.  A wavefront keeps the best so far sorted over its lanes, as 64-bit keys (value, then the
-// lower index) whose order is that of whole numbers; a class is looked at only if its value reaches that of the last one
-// kept, which after the first few tiles hardly any does, so the price is a comparison for every 16 classes.
+// lower index) whose order is that of whole numbers.  Every 32 tiles it picks out what reaches the n_top-th of its lanes'
+// largest values: hardly more than n_top classes, so the price is a maximum and a store to LDS for every 16 classes.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <climits>
+#include <type_traits>
 
 #define CNN_GLOBAL __attribute__((address_space(1)))
 #include "cnn355_ops.h"
@@ -42,28 +42,90 @@ __device__ __forceinline__ u64 key_of(float v, int index) {
   const unsigned b = __builtin_bit_cast(unsigned, v + 0.0f);   // (-0 as 0)
   return (u64)((int)b < 0 ? ~b : b | 0x80000000u) << 32 | (unsigned)~index;
 }
+__device__ __forceinline__ u64 key_of_any(float v, int index) { return v == v ? key_of(v, index) : 0; }   // (0: no number)
 __device__ __forceinline__ int index_of(u64 k) { return (int)~(unsigned)k; }
 __device__ __forceinline__ float value_of(u64 k) {
   const unsigned b = (unsigned)(k >> 32);
   return __builtin_bit_cast(float, (int)b < 0 ? b & 0x7fffffffu : ~b);
 }
 
-template <class T>
-__device__ __forceinline__ T larger(T a, T b) { return a < b ? b : a; }
-template <class T>
-__device__ __forceinline__ T smaller(T a, T b) { return a < b ? a : b; }
+// ---- between lanes, without LDS ----
+// a word of the lane whose number differs by D (a power of two)
+template <int D>
+__device__ __forceinline__ unsigned xor_word(unsigned v) {
+  if constexpr (D == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true);        // quad_perm [1, 0, 3, 2]
+  else if constexpr (D == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true);   // quad_perm [2, 3, 0, 1]
+  else if constexpr (D == 4)                                                             // row_half_mirror, quad_perm [3, 2, 1, 0]
+    return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true), 0x1B, 0xf, 0xf, true);
+  else if constexpr (D == 8) return __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);  // row_ror:8
+  else if constexpr (D == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
+}
+template <int D>
+__device__ __forceinline__ float xor_lane(float v) { return __builtin_bit_cast(float, xor_word<D>(__builtin_bit_cast(unsigned, v))); }
+template <int D>
+__device__ __forceinline__ u64 xor_lane(u64 v) { return (u64)xor_word<D>((unsigned)(v >> 32)) << 32 | xor_word<D>((unsigned)v); }
 
-// Values of `lanes` lanes side by side (a power of two) in descending order; `from` > 2: they already are in two runs of
-// lanes, rising and falling or the other way round, of which only the merge is left (from = lanes).
+// f(a constant) for 1, 2, 4, .. below LANES
+template <int LANES, class F>
+__device__ __forceinline__ void for_distances(F f) {
+  if constexpr (LANES > 1) f(std::integral_constant<int, 1>());
+  if constexpr (LANES > 2) f(std::integral_constant<int, 2>());
+  if constexpr (LANES > 4) f(std::integral_constant<int, 4>());
+  if constexpr (LANES > 8) f(std::integral_constant<int, 8>());
+  if constexpr (LANES > 16) f(std::integral_constant<int, 16>());
+  if constexpr (LANES > 32) f(std::integral_constant<int, 32>());
+}
+
+// Bitonic sorting: groups of LANES lanes that rise and then fall, or the other way round, in falling order, every second one
+// in rising order.
+template <int LANES, int D, class T>
+__device__ __forceinline__ T merge_steps(T v) {
+  if constexpr (D >= 1) {
+    const int lane = threadIdx.x & 63;
+    const T o = xor_lane<D>(v);
+    const bool want_larger = ((lane & D) == 0) == ((lane & LANES) == 0);
+    v = (v < o) == want_larger ? o : v;   // (equal ones: either)
+    return merge_steps<LANES, D / 2>(v);
+  } else {
+    return v;
+  }
+}
+// ... of any groups
+template <int LANES, class T>
+__device__ __forceinline__ T sort_steps(T v) {
+  if constexpr (LANES > 2) v = sort_steps<LANES / 2>(v);
+  return merge_steps<LANES, LANES / 2>(v);
+}
+// ... all of them in falling order
+template <int D, class T>
+__device__ __forceinline__ T fall_steps(T v) {
+  if constexpr (D >= 1) {
+    const T o = xor_lane<D>(v);
+    v = (v < o) == ((threadIdx.x & D) == 0) ? o : v;
+    return fall_steps<D / 2>(v);
+  } else {
+    return v;
+  }
+}
+// every group of LANES lanes in falling order
+template <int LANES, class T>
+__device__ __forceinline__ T sort_lanes(T v) {
+  if constexpr (LANES > 2) v = sort_steps<LANES / 2>(v);
+  return fall_steps<LANES / 2>(v);
+}
+// the larger ones of two sorted runs of 64, sorted: the second one comes in rising order
 template <class T>
-__device__ __forceinline__ T sort_lanes(T v, int lanes, int from = 2) {
-  const int lane = threadIdx.x & 63;
-  for (int size = from; size <= lanes; size <<= 1)
-    for (int d = size >> 1; d; d >>= 1) {
-      const T o = __shfl_xor(v, d);
-      const bool first = (lane & d) == 0, down = size == lanes || (lane & size) == 0;
-      v = first == down ? larger(v, o) : smaller(v, o);
-    }
+__device__ __forceinline__ T best_of(T falling, T rising) { return fall_steps<32>(falling < rising ? rising : falling); }
+// sorted the other way round
+template <class T>
+__device__ __forceinline__ T reversed(T v) {
+  for_distances<64>([&](auto d) { v = xor_lane<decltype(d)::value>(v); });
   return v;
 }
 
@@ -80,11 +142,15 @@ __device__ __forceinline__ void lift(Sums& a, float m) {
   a.m = m;
 }
 
-__device__ __forceinline__ void join_lanes(Sums& a, int lanes) {
+template <int LANES>
+__device__ __forceinline__ void join_lanes(Sums& a) {
   float m = a.m;
-  for (int d = 1; d < lanes; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  for_distances<LANES>([&](auto d) { m = fmaxf(m, xor_lane<decltype(d)::value>(m)); });
   lift(a, m);
-  for (int d = 1; d < lanes; d <<= 1) { a.s += __shfl_xor(a.s, d); a.t += __shfl_xor(a.t, d); }
+  for_distances<LANES>([&](auto d) {
+    a.s += xor_lane<decltype(d)::value>(a.s);
+    a.t += xor_lane<decltype(d)::value>(a.t);
+  });
 }
 
 // What a row's sums come to.  A row without a value above -inf is empty; one with +inf or NaN has no distribution.
@@ -127,7 +193,14 @@ __device__ __forceinline__ void give_row(const ScoreJob& J, long long row, int l
 }
 
 // ---- the best classes of a wavefront ----
-constexpr int HELD = 128;   // keys waiting in LDS: fewer than 64, and those of one look at every lane
+constexpr int SEGMENT = 32;  // tiles after which a wavefront picks out the best
+constexpr int HELD = 128;    // keys, or tiles' lanes, waiting in LDS: fewer than 64, and those of one look at every lane
+
+struct Picking {             // LDS of a wavefront
+  u64 held[HELD];
+  unsigned short where[HELD];          // tile of the segment, lane
+  unsigned short largest[SEGMENT][64]; // of every lane's 16 classes of a tile the largest, upper half of a float, rounded up
+};
 
 struct Best {
   u64 list;        // lane i: the i-th best so far, 0: none
@@ -142,108 +215,205 @@ __device__ __forceinline__ u64 lane_of(u64 v, int lane) {
 __device__ __forceinline__ float lane_of(float v, int lane) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
+__device__ __forceinline__ int place_in(u64 lanes) { return __builtin_amdgcn_mbcnt_hi((unsigned)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)lanes, 0)); }
+__device__ __forceinline__ void lds_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }   // (a wavefront's own lanes)
 
 // the 64 (or fewer) keys in front join the list
-__device__ __forceinline__ void take_held(Best& b, u64* held, int n_top) {
+__device__ __forceinline__ void take_held(Best& b, Picking& L, int n_top) {
   const int lane = threadIdx.x & 63;
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  const u64 mine = lane < b.held ? held[lane] : 0, rest = 64 + lane < b.held ? held[64 + lane] : 0;
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  held[lane] = rest;
+  lds_order();
+  const u64 mine = lane < b.held ? L.held[lane] : 0, rest = 64 + lane < b.held ? L.held[64 + lane] : 0;
+  lds_order();
+  L.held[lane] = rest;
   b.held = b.held > 64 ? b.held - 64 : 0;
-  const u64 sorted = sort_lanes(mine, 64);
-  b.list = sort_lanes(larger(b.list, (u64)__shfl(sorted, 63 - lane)), 64, 64);
+  b.list = best_of(b.list, reversed(sort_lanes<64>(mine)));
   const u64 last = lane_of(b.list, n_top - 1);
-  // (the classes of the tiles to come have higher indices: of theirs, only larger values are above that key)
-  if (last > b.bar) { b.bar = last; b.bar_value = value_of(last + (1ull << 32)); }
+  if (last > b.bar) {
+    // (the classes of the tiles to come have higher indices: of theirs, only larger values are above that key)
+    b.bar = last;
+    b.bar_value = value_of(last + (1ull << 32));
+  }
 }
 
-// A tile of a wavefront, x[k] of class first + (k / V) 64 V + lane V + k % V, `largest` the lane's largest, `end` the
-// first class that is not the row's (or its part's).
+// Rows are looked at from the 16 bytes on that their first class lies in: place 0 is `lead` classes in front of it, and `end`
+// the first place behind the last.  (Loads of 16 bytes at odd addresses cost a row of 131071 bf16 classes 13 %.)
 template <int TYPE>
-__device__ __forceinline__ void look(Best& b, u64* held, const CNN_GLOBAL typename Element<TYPE>::T* row, const float (&x)[16],
-                                     float largest, int first, int end, int n_top) {
+struct RowAt {
+  const CNN_GLOBAL typename Element<TYPE>::T* at;   // place 0
+  int lead, end;
+};
+template <int TYPE>
+__device__ __forceinline__ RowAt<TYPE> row_at(const ScoreJob& J, long long row) {
+  typedef typename Element<TYPE>::T T;
+  const CNN_GLOBAL T* x = (const CNN_GLOBAL T*)J.x + row * J.stride;
+  const int lead = (int)((unsigned long long)x & 15) / (int)sizeof(T);
+  return RowAt<TYPE>{x - lead, lead, J.classes + lead};
+}
+
+// The best of a segment: tiles first, first + step, ... of a row, of which place (k / V) 64 V + lane V + k % V is a lane's k-th.
+// m0, m1: the largest values of the first and second half of every lane's classes, in this segment and those before it.
+//
+// As many classes as are asked for reach the n_top-th of the lanes' largest values, so what lies below it is out.  Of G such
+// values and n_top best G log(G / (G - n_top)) classes reach it where their order is chance: 24 of 64 for 20, 89 of 128 for 64
+// (and 300 of 64).  Their classes are asked for again, one to a lane, 16 lanes' at a time.
+// (Looking at every tile as it comes, against the best so far, finds some in every second tile of a row of 131072: 4096 such
+// rows with 20 best took 252 us so, 194 without any best.)
+template <int TYPE>
+__device__ __forceinline__ void pick(Best& b, Picking& L, const RowAt<TYPE>& row, float m0, float m1, int first, int step, int tiles, int n_top) {
   typedef Element<TYPE> E;
   constexpr int V = E::V;
-  const u64 any = __ballot(largest >= b.bar_value);
-  if (!any) return;
   const int lane = threadIdx.x & 63;
-  // Many lanes at once, as in a wavefront's first tile or where values rise along the row: as many classes as are asked for
-  // reach the n_top-th of the lanes' largest values, so what lies below it is out.
-  if (b.bar == 0 || __popcll(any) > n_top) {
-    const float v = lane_of(sort_lanes(largest, 64), n_top - 1);
-    if (v > b.bar_value) { b.bar_value = v; b.bar = key_of(v, -1); }
+  const float v = lane_of(n_top <= 24 ? sort_lanes<64>(fmaxf(m0, m1)) : best_of(sort_lanes<64>(m0), reversed(sort_lanes<64>(m1))), n_top - 1);
+  if (v > LOWEST && v > b.bar_value) {   // (LOWEST: lanes without any)
+    b.bar_value = v;
+    b.bar = key_of(v, -1);
   }
-  unsigned hits = 0;
+  int waiting = 0;
+  for (int i = 0; i < tiles; ++i) {
+    const u64 in = __ballot(__builtin_bit_cast(float, (unsigned)L.largest[i][lane] << 16) >= b.bar_value);
+    if (in) {
+      if (in >> lane & 1) L.where[waiting + place_in(in)] = (unsigned short)(i << 6 | lane);
+      waiting += __popcll(in);
+    }
+    if (waiting < 64 && i + 1 < tiles) continue;
+    lds_order();
+    for (int w0 = 0; w0 < waiting; w0 += 16) {
+      u64 key[4];
 #pragma unroll
-  for (int k = 0; k < 16; ++k) hits |= x[k] >= b.bar_value ? 1u << k : 0u;
-  while (__ballot(hits != 0)) {
-    const int k = __builtin_ctz(hits | 0x10000u), at = first + (k / V) * 64 * V + lane * V + k % V;
-    u64 key = 0;
-    if (hits && at < end) key = key_of(E::get(row[at]), at);   // (asked for again: it has just been read)
-    hits &= hits - 1;
-    const u64 in = __ballot(key > b.bar);
-    if (key > b.bar) held[b.held + __builtin_amdgcn_mbcnt_hi((unsigned)(in >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in, 0))] = key;
-    b.held += __popcll(in);
-    if (b.held >= 64) take_held(b, held, n_top);
+      for (int u = 0; u < 4; ++u) {
+        const int w = w0 + u * 4 + (lane >> 4), k = lane & 15;
+        const int at_lane = w < waiting ? L.where[w] : 0;
+        const int at = (first + (at_lane >> 6) * step) * SCORE_TILE + (k / V) * 64 * V + (at_lane & 63) * V + k % V;
+        key[u] = w < waiting && at >= row.lead && at < row.end ? key_of_any(E::get(row.at[at]), at - row.lead) : 0;
+      }
+#pragma unroll 1
+      for (int u = 0; u < 4; ++u) {
+        const u64 k = u == 0 ? key[0] : u == 1 ? key[1] : u == 2 ? key[2] : key[3];
+        const u64 take = __ballot(k > b.bar);
+        if (!take) continue;
+        if (k > b.bar) L.held[b.held + place_in(take)] = k;
+        b.held += __popcll(take);
+        if (b.held >= 64) take_held(b, L, n_top);
+      }
+    }
+    waiting = 0;
+    lds_order();
   }
 }
 
 // ---- the pass over a row ----
+template <int TYPE>
+__device__ __forceinline__ void load_tile(v4u (&r)[16 / Element<TYPE>::V], const RowAt<TYPE>& row, int tile) {
+  constexpr int V = Element<TYPE>::V, N = 16 / V;
+  const int lane = threadIdx.x & 63, first = tile * SCORE_TILE;
+  const CNN_GLOBAL typename Element<TYPE>::T* at = row.at + first;
+  if (first >= row.lead && first + SCORE_TILE <= row.end) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) r[q] = *(const CNN_GLOBAL v4u*)(at + (q * 64 + lane) * V);
+  } else {
+#pragma unroll
+    for (int q = 0; q < N; ++q) r[q] = load16<TYPE>(at, (q * 64 + lane) * V, row.end - first, row.lead - first);
+  }
+}
+
 // Tiles first, first + step, ... of a row, below `last`: the wavefront's sums, lane by lane, and its best.
+//
+// In the usual tile the exponent is one operation, d = x / ln 2 - r with r = m / ln 2 as rounded: every e is too large by the
+// same 2^(m / ln 2 - r), which is taken out at the end.  A masked class gives 0 (-inf) there and values near the type's lowest
+// and highest leave the range of d; a tile that has any shows it in its sums, is done again with d = (x - m) / ln 2 and the
+// product of e and d clamped, and so are those behind it (two operations more for each class).
 template <int TYPE, bool ENTROPY, bool TOP>
-__device__ __forceinline__ void scan(const ScoreJob& J, const CNN_GLOBAL typename Element<TYPE>::T* row, int first, int step, int last,
-                                     Sums& a, Best& b, u64* held) {
+__device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step, int last, int n_top, Sums& a, Best& b, Picking* L) {
   typedef Element<TYPE> E;
   constexpr int V = E::V, N = 16 / V;
-  const int lane = threadIdx.x & 63, end = J.classes;
   a = Sums{LOWEST, 0.0f, 0.0f};
   b = Best{0, 0, -INFINITY, 0};
+  float r = -INFINITY;
+  float largest[2] = {LOWEST, LOWEST};
+  bool rough = false;
+  auto settle = [&]() {   // sums of 2^(x / ln 2 - r) to sums of 2^((x - m) / ln 2)
+    if (a.s > 0.0f) {
+      const float off = fmaf(a.m, LOG2E, -r), f = __builtin_amdgcn_exp2f(-off);
+      a.t = fmaf(-off, a.s, a.t) * f;
+      a.s *= f;
+    }
+  };
   v4u next[N];
-  if (first < last) {
-#pragma unroll
-    for (int q = 0; q < N; ++q) next[q] = load16<TYPE>(row, first * SCORE_TILE + q * 64 * V + lane * V, end);
-  }
+  if (first < last) load_tile<TYPE>(next, row, first);
+  int in_segment = 0;
   for (int tile = first; tile < last; tile += step) {
     float x[16];
 #pragma unroll
     for (int k = 0; k < 16; ++k) x[k] = E::get(next[k / V], k % V);
-    if (tile + step < last) {
+    if (tile + step < last) load_tile<TYPE>(next, row, tile + step);
+    float top[2];
 #pragma unroll
-      for (int q = 0; q < N; ++q) next[q] = load16<TYPE>(row, (tile + step) * SCORE_TILE + q * 64 * V + lane * V, end);
+    for (int h = 0; h < 2; ++h) {
+      top[h] = max3(x[8 * h], x[8 * h + 1], x[8 * h + 2]);
+      top[h] = max3(top[h], x[8 * h + 3], x[8 * h + 4]);
+      top[h] = max3(top[h], x[8 * h + 5], x[8 * h + 6]);
+      top[h] = max3(top[h], x[8 * h + 7], x[8 * h + 7]);
+      if (TOP) largest[h] = max3(largest[h], top[h], top[h]);
     }
-    float largest = max3(x[0], x[1], x[2]);
+    const float m = max3(a.m, top[0], top[1]);
+    if (!rough) {
+      const float to = m * LOG2E, d0 = r - to, f = __builtin_amdgcn_exp2f(d0);
+      float s = a.s * f, t = fmaf(fmaxf(d0, FAR), a.s, a.t) * f;
 #pragma unroll
-    for (int k = 3; k < 15; k += 2) largest = max3(largest, x[k], x[k + 1]);
-    largest = max3(largest, x[15], x[15]);
-    lift(a, max3(a.m, largest, largest));
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      const float d = (x[k] - a.m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
-      a.s += e;
-      if (ENTROPY) a.t = fmaf(e, fmaxf(d, FAR), a.t);
+      for (int k = 0; k < 16; ++k) {
+        const float d = fmaf(x[k], LOG2E, -to), e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        if (ENTROPY) t = fmaf(e, d, t);
+      }
+      const float sure = ENTROPY ? t : s;
+      if (__ballot(!(sure - sure == 0.0f)) == 0) {
+        r = to;
+        a = Sums{m, s, t};
+      } else {
+        rough = true;
+        settle();
+      }
     }
-    if (TOP) look<TYPE>(b, held, row, x, largest, tile * SCORE_TILE, end, J.n_top);
+    if (rough) {
+      lift(a, m);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const float d = (x[k] - a.m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+        a.s += e;
+        if (ENTROPY) a.t = fmaf(e, fmaxf(d, FAR), a.t);
+      }
+    }
+    if (TOP) {
+      const unsigned bits = __builtin_bit_cast(unsigned, max3(top[0], top[1], top[1]));
+      L->largest[in_segment++][threadIdx.x & 63] = (unsigned short)((TYPE == ELEMENT_BF16 || (int)bits < 0 ? bits : bits + 0xffffu) >> 16);
+      if (in_segment == SEGMENT || tile + step >= last) {
+        pick<TYPE>(b, *L, row, largest[0], largest[1], tile - (in_segment - 1) * step, step, in_segment, n_top);
+        in_segment = 0;
+      }
+    }
   }
-  if (TOP && b.held) take_held(b, held, J.n_top);
+  if (!rough) settle();
+  if (TOP && b.held) take_held(b, *L, n_top);
 }
 
 // Rows of more than 64 classes, WAVES wavefronts a row or, where parts > 1, a part of one.
 template <int TYPE, int WAVES, bool ENTROPY, bool TOP>
 __global__ void __launch_bounds__(ST) k_scores(ScoreJob J) {
   constexpr int ROWS = ST / 64 / WAVES;
-  __shared__ u64 lds_held[TOP ? ST / 64 : 1][HELD];
+  __shared__ Picking lds_picking[TOP ? ST / 64 : 1];
   __shared__ u64 lds_best[TOP && WAVES > 1 ? WAVES : 1][64];
   __shared__ float lds_sums[WAVES][4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part_of = WAVES > 1 ? 0 : wave, w = WAVES > 1 ? wave : 0;
-  const int part = blockIdx.y, tiles = (J.classes + SCORE_TILE - 1) / SCORE_TILE;
+  const int part = blockIdx.y;
   for (long long row = (long long)blockIdx.x * ROWS + part_of; row < J.rows; row += (long long)gridDim.x * ROWS) {
     Sums a;
     Best b;
-    scan<TYPE, ENTROPY, TOP>(J, (const CNN_GLOBAL typename Element<TYPE>::T*)J.x + row * J.stride, part * J.part_tiles + w, WAVES,
-                             min(tiles, (part + 1) * J.part_tiles), a, b, lds_held[TOP ? wave : 0]);
-    join_lanes(a, 64);
+    const RowAt<TYPE> x = row_at<TYPE>(J, row);
+    const int tiles = (x.end + SCORE_TILE - 1) / SCORE_TILE;   // (one more than the parts were planned for, it may be)
+    scan<TYPE, ENTROPY, TOP>(x, part * J.part_tiles + w, WAVES, part + 1 == J.parts ? tiles : (part + 1) * J.part_tiles, J.n_top, a, b,
+                             &lds_picking[TOP ? wave : 0]);
+    join_lanes<64>(a);
     if (WAVES > 1) {
       __syncthreads();   // (what the row before left has been read)
       if (lane == 0) { lds_sums[w][0] = a.m; lds_sums[w][1] = a.s; lds_sums[w][2] = a.t; }
@@ -252,9 +422,9 @@ __global__ void __launch_bounds__(ST) k_scores(ScoreJob J) {
       if (wave != 0) continue;
       a = Sums{LOWEST, 0.0f, 0.0f};
       if (lane < WAVES) a = Sums{lds_sums[lane][0], lds_sums[lane][1], lds_sums[lane][2]};
-      join_lanes(a, 64);
+      join_lanes<64>(a);
       if (TOP)
-        for (int o = 1; o < WAVES; ++o) b.list = sort_lanes(larger(b.list, lds_best[o][63 - lane]), 64, 64);
+        for (int o = 1; o < WAVES; ++o) b.list = best_of(b.list, lds_best[o][63 - lane]);
     }
     if (J.parts > 1) {
       const long long at = row * J.parts + part;
@@ -281,12 +451,12 @@ __global__ void __launch_bounds__(ST) k_scores_join(ScoreJob J) {
       const CNN_GLOBAL float* p = J.part_sums + (row * J.parts + threadIdx.x) * 4;
       a = Sums{p[0], p[1], p[2]};
     }
-    join_lanes(a, 64);
+    join_lanes<64>(a);
     u64 list = 0;
     if (J.n_top)
       for (int part = wave; part < J.parts; part += ST / 64) {
         const u64 k = 63 - lane < J.n_top ? J.part_best[(row * J.parts + part) * J.n_top + 63 - lane] : 0;
-        list = sort_lanes(larger(list, k), 64, 64);
+        list = best_of(list, k);
       }
     __syncthreads();
     if (lane == 0) { lds_sums[wave][0] = a.m; lds_sums[wave][1] = a.s; lds_sums[wave][2] = a.t; }
@@ -295,9 +465,9 @@ __global__ void __launch_bounds__(ST) k_scores_join(ScoreJob J) {
     if (wave != 0) continue;
     a = Sums{LOWEST, 0.0f, 0.0f};
     if (lane < ST / 64) a = Sums{lds_sums[lane][0], lds_sums[lane][1], lds_sums[lane][2]};
-    join_lanes(a, 64);
+    join_lanes<64>(a);
     if (J.n_top)
-      for (int o = 1; o < ST / 64; ++o) list = sort_lanes(larger(list, lds_best[o][63 - lane]), 64, 64);
+      for (int o = 1; o < ST / 64; ++o) list = best_of(list, lds_best[o][63 - lane]);
     give_row<TYPE>(J, row, lane, a, list);
   }
 }
@@ -312,12 +482,15 @@ __global__ void __launch_bounds__(ST) k_scores_few(ScoreJob J) {
     const bool is = row < J.rows && c < J.classes;
     const float x = is ? E::get(((const CNN_GLOBAL typename E::T*)J.x)[row * J.stride + c]) : -INFINITY;
     float m = fmaxf(x, LOWEST);
-    for (int d = 1; d < L; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+    for_distances<L>([&](auto d) { m = fmaxf(m, xor_lane<decltype(d)::value>(m)); });
     const float d = (x - m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
     Sums a{m, e, e * fmaxf(d, FAR)};
-    for (int o = 1; o < L; o <<= 1) { a.s += __shfl_xor(a.s, o); a.t += __shfl_xor(a.t, o); }
-    u64 k = is && x == x ? key_of(x, c) : 0;
-    if (J.n_top) k = sort_lanes(k, L);
+    for_distances<L>([&](auto o) {
+      a.s += xor_lane<decltype(o)::value>(a.s);
+      a.t += xor_lane<decltype(o)::value>(a.t);
+    });
+    u64 k = is ? key_of_any(x, c) : 0;
+    if (J.n_top) k = sort_lanes<L>(k);
     if (row < J.rows) give_row<TYPE>(J, row, c, a, k);
   }
 }
