@@ -153,62 +153,63 @@ def deform_images(d_src, d_dst, n, params, seed, first_index, d_src_index=None, 
         raise CnnError(rc, "cnn_deform_images", _err())
 
 
+_kinds, _f32, _i32, _u8, _current_device, _raw_stream, _device_guard = {}, None, None, None, None, None, None
+
+
+def _know_torch():
+    """What the calls below ask of torch, looked up once: they take a few microseconds on the device."""
+    global _kinds, _f32, _i32, _u8, _current_device, _raw_stream, _device_guard
+    import torch
+    _f32, _i32, _u8 = torch.float32, torch.int32, torch.uint8
+    _current_device, _device_guard = torch.cuda.current_device, torch.cuda.device
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    _kinds = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+
+
 def _element_type(t):
     """TYPE_* of a tensor."""
-    import torch
-    kinds = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
-    assert t.dtype in kinds, "expected float32, bfloat16 or float16"
-    return kinds[t.dtype]
+    if not _kinds:
+        _know_torch()
+    assert t.dtype in _kinds, "expected float32, bfloat16 or float16"
+    return _kinds[t.dtype]
 
 
-def _f32_of(t, shape, device):
-    """Address of a contiguous float32 tensor of this shape (None: None)."""
-    import torch
+def _address(t, kind, shape, device):
+    """Address of a contiguous tensor of this type and shape (None: None)."""
     if t is None:
         return None
-    assert t.device == device and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == shape, \
-        "expected a contiguous float32 tensor %r on %s" % (shape, device)
-    return t.data_ptr()
-
-
-def _labels_of(t, rows, device):
-    import torch
-    if t is None:
-        return None
-    assert t.device == device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == rows
+    assert t.dtype == kind and t.shape == shape and t.device == device and t.is_contiguous(), \
+        "expected a contiguous %s tensor %r on %s" % (kind, tuple(shape), device)
     return t.data_ptr()
 
 
 def _rows_of(t):
     """(address, type, rows, classes, elements between rows) of a matrix whose rows are contiguous."""
+    kind = _element_type(t)
     assert t.is_cuda and t.dim() == 2, "expected a device matrix"
     rows, classes = t.shape
-    assert classes <= 1 or t.stride(1) == 1, "the elements of a row must lie side by side"
-    return t.data_ptr(), _element_type(t), rows, classes, max(t.stride(0), classes) if rows <= 1 else t.stride(0)
+    stride, across = t.stride()
+    assert classes <= 1 or across == 1, "the elements of a row must lie side by side"
+    return t.data_ptr(), kind, rows, classes, max(stride, classes) if rows <= 1 else stride
 
 
 def _scratch_of(t, device):
-    import torch
     if t is None or t.numel() == 0:
         return None, 0
-    assert t.device == device and t.dtype == torch.uint8 and t.is_contiguous()
+    assert t.dtype == _u8 and t.device == device and t.is_contiguous()
     return t.data_ptr(), t.numel()
 
 
-class _On:
-    """The device of a call's tensors made the current one, and the stream it is issued on."""
-
-    def __init__(self, device, stream):
-        import torch
-        self._guard = torch.cuda.device(device)
-        self.stream = (stream or torch.cuda.current_stream(device)).cuda_stream
-
-    def __enter__(self):
-        self._guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *e):
-        return self._guard.__exit__(*e)
+def _on(device, stream, call, *args):
+    """call(stream, *args) with the device of its tensors the current one."""
+    if stream is not None:
+        raw = stream.cuda_stream
+    else:
+        raw = _raw_stream(device.index)
+    if _current_device() == device.index:
+        return call(raw, *args)
+    with _device_guard(device):
+        return call(raw, *args)
 
 
 def class_scores_scratch_bytes(rows, classes, n_top=0):
@@ -226,20 +227,15 @@ def class_scores(d_logits, d_labels=None, d_log_probs=None, d_entropy=None, d_no
     outputs (each of them or None) float32 d_log_probs [rows], d_entropy [rows], d_normaliser [rows][2], int32 d_top and
     float32 d_top_log_probs [rows][n_top]; d_scratch: uint8, class_scores_scratch_bytes(rows, classes, n_top) of it.
     Asynchronous on `stream` (a torch stream; None: the current)."""
-    import torch
     x, kind, rows, classes, stride = _rows_of(d_logits)
     dev = d_logits.device
-    n_top = 0
-    if d_top is not None:
-        n_top = d_top.shape[1]
-        assert d_top.device == dev and d_top.dtype == torch.int32 and d_top.is_contiguous() and tuple(d_top.shape) == (rows, n_top)
-    elif d_top_log_probs is not None:
-        n_top = d_top_log_probs.shape[1]
+    some = d_top if d_top is not None else d_top_log_probs
+    n_top = 0 if some is None else some.shape[-1]
     scratch, nbytes = _scratch_of(d_scratch, dev)
-    with _On(dev, stream) as s:
-        rc = lib().cnn_class_scores(s, x, kind, rows, classes, stride, _labels_of(d_labels, rows, dev), _f32_of(d_log_probs, (rows,), dev),
-                                    _f32_of(d_entropy, (rows,), dev), _f32_of(d_normaliser, (rows, 2), dev), n_top,
-                                    None if d_top is None else d_top.data_ptr(), _f32_of(d_top_log_probs, (rows, n_top), dev), scratch, nbytes)
+    each, best = (rows,), (rows, n_top)
+    rc = _on(dev, stream, lib().cnn_class_scores, x, kind, rows, classes, stride, _address(d_labels, _i32, each, dev),
+             _address(d_log_probs, _f32, each, dev), _address(d_entropy, _f32, each, dev), _address(d_normaliser, _f32, (rows, 2), dev),
+             n_top, _address(d_top, _i32, best, dev), _address(d_top_log_probs, _f32, best, dev), scratch, nbytes)
     if rc:
         raise CnnError(rc, "cnn_class_scores", _err())
 
@@ -249,12 +245,11 @@ def class_scores_grad(d_logits, d_grad, d_normaliser, d_labels=None, d_g_log_pro
     sum(d_g_log_probs * log_probs) + sum(d_g_entropy * entropy); d_normaliser and d_entropy as class_scores gave them."""
     x, kind, rows, classes, stride = _rows_of(d_logits)
     g, g_kind, g_rows, g_classes, g_stride = _rows_of(d_grad)
-    dev = d_logits.device
-    assert d_grad.device == dev and g_kind == kind and (g_rows, g_classes) == (rows, classes)
-    with _On(dev, stream) as s:
-        rc = lib().cnn_class_scores_grad(s, x, kind, rows, classes, stride, _labels_of(d_labels, rows, dev), _f32_of(d_normaliser, (rows, 2), dev),
-                                         _f32_of(d_entropy, (rows,), dev), _f32_of(d_g_log_probs, (rows,), dev),
-                                         _f32_of(d_g_entropy, (rows,), dev), g, g_stride)
+    dev, each = d_logits.device, (rows,)
+    assert d_grad.device == dev and (g_kind, g_rows, g_classes) == (kind, rows, classes)
+    rc = _on(dev, stream, lib().cnn_class_scores_grad, x, kind, rows, classes, stride, _address(d_labels, _i32, each, dev),
+             _address(d_normaliser, _f32, (rows, 2), dev), _address(d_entropy, _f32, each, dev), _address(d_g_log_probs, _f32, each, dev),
+             _address(d_g_entropy, _f32, each, dev), g, g_stride)
     if rc:
         raise CnnError(rc, "cnn_class_scores_grad", _err())
 
@@ -285,13 +280,15 @@ class TensorList:
 
 def _dense_order(t):
     """((size, stride) of the dimensions of more than one element) of a tensor without gaps; an error of any other."""
+    if t.is_contiguous():
+        return ()
     dims = [(n, s) for n, s in zip(t.shape, t.stride()) if n != 1]
     at = 1
     if t.numel():
         for n, s in sorted(dims, key=lambda d: d[1]):
             assert s == at, "expected a tensor without gaps"
             at *= n
-    return () if t.is_contiguous() else tuple(dims)
+    return tuple(dims)
 
 
 def gradient_scratch_bytes(n):
@@ -303,40 +300,41 @@ def gradient_scratch_bytes(n):
     return b.value
 
 
-def _over_gradients(grads, other, d_norm, d_scratch, stream, call):
-    import torch
+def _over_gradients(grads, other, d_norm, d_scratch):
+    """(device, address of the norm, scratch, its bytes) of a call, its lists looked over."""
+    if _f32 is None:
+        _know_torch()
     dev = grads.device or (d_norm if d_norm is not None else d_scratch).device
     if other is not None:
-        assert len(other) == len(grads) and (other.device == dev or not len(grads)) and other.orders == grads.orders, \
+        assert len(other) == len(grads) and other.device == grads.device and other.orders == grads.orders, \
             "lists that go together have the same tensors, laid out alike"
-    assert d_norm is None or (d_norm.device == dev and d_norm.dtype == torch.float32 and d_norm.numel() == 1)
-    scratch, nbytes = _scratch_of(d_scratch, dev)
-    with _On(dev, stream) as s:
-        rc = call(s, None if d_norm is None else d_norm.data_ptr(), scratch, nbytes)
-    if rc:
-        raise CnnError(rc, call.__name__, _err())
+    assert d_norm is None or (d_norm.dtype == _f32 and d_norm.numel() == 1 and d_norm.device == dev)
+    return (dev, None if d_norm is None else d_norm.data_ptr()) + _scratch_of(d_scratch, dev)
 
 
 def gradient_norm(grads, d_norm, d_scratch, stream=None):
     """cnn_gradient_norm: d_norm (one float32) = the 2-norm over all elements of all tensors of a TensorList; d_scratch: uint8,
     gradient_scratch_bytes(len(grads)) of it."""
-    def cnn_gradient_norm(s, norm, scratch, nbytes):
-        return lib().cnn_gradient_norm(s, grads.array, len(grads), norm, scratch, nbytes)
-    _over_gradients(grads, None, d_norm, d_scratch, stream, cnn_gradient_norm)
+    dev, norm, scratch, nbytes = _over_gradients(grads, None, d_norm, d_scratch)
+    rc = _on(dev, stream, lib().cnn_gradient_norm, grads.array, len(grads), norm, scratch, nbytes)
+    if rc:
+        raise CnnError(rc, "cnn_gradient_norm", _err())
 
 
 def clip_gradients(grads, max_norm, d_scratch, out=None, d_norm=None, stream=None):
     """cnn_clip_gradients: the gradients, in place or into the TensorList `out`, scaled to a norm of at most max_norm."""
-    def cnn_clip_gradients(s, norm, scratch, nbytes):
-        return lib().cnn_clip_gradients(s, grads.array, None if out is None else out.array, len(grads), float(max_norm), norm, scratch, nbytes)
-    _over_gradients(grads, out, d_norm, d_scratch, stream, cnn_clip_gradients)
+    dev, norm, scratch, nbytes = _over_gradients(grads, out, d_norm, d_scratch)
+    rc = _on(dev, stream, lib().cnn_clip_gradients, grads.array, None if out is None else out.array, len(grads), max_norm, norm, scratch, nbytes)
+    if rc:
+        raise CnnError(rc, "cnn_clip_gradients", _err())
 
 
 def clipped_update(weights, grads, lr, max_norm, d_scratch, d_norm=None, stream=None):
     """cnn_clipped_update: weights (float32) -= lr * factor * grads, the factor that of clip_gradients."""
-    def cnn_clipped_update(s, norm, scratch, nbytes):
-        return lib().cnn_clipped_update(s, weights.array, grads.array, len(grads), float(lr), float(max_norm), norm, scratch, nbytes)
-    _over_gradients(grads, weights, d_norm, d_scratch, stream, cnn_clipped_update)
+    dev, norm, scratch, nbytes = _over_gradients(grads, weights, d_norm, d_scratch)
+    rc = _on(dev, stream, lib().cnn_clipped_update, weights.array, grads.array, len(grads), lr, max_norm, norm, scratch, nbytes)
+    if rc:
+        raise CnnError(rc, "cnn_clipped_update", _err())
 
 
 def deform_on_matrix_cores(maps, rows, cols, sigma):

@@ -324,6 +324,7 @@ __device__ __forceinline__ void load_tile(v4u (&r)[16 / Element<TYPE>::V], const
 // product of e and d clamped, and so are those behind it (two operations more for each class).
 template <int TYPE, bool ENTROPY, bool TOP>
 __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step, int last, int n_top, Sums& a, Best& b, Picking* L) {
+#pragma clang fp contract(off)   // (r is the rounded product in the difference of two of them, too)
   typedef Element<TYPE> E;
   constexpr int V = E::V, N = 16 / V;
   a = Sums{LOWEST, 0.0f, 0.0f};
@@ -577,6 +578,15 @@ int lanes_of(int classes) {
   return l;
 }
 
+// One wavefront a row or four: four share what is read, but each picks out its own best, and the lists have to be joined.
+// us of one / four with 20 best, bf16: 2048 rows of 8192 classes 15 / 22, 20000 91 / 186; 4096 rows of 32768 65 / 78, 1024 27 / 22;
+// of 131072 4096 rows 209 / 218, 5000 (one of two rounds a fifth full) 305 / 264.  Without best, fp32: 20000 rows of 4096 59 / 64,
+// of 8192 113 / 109, of 32768 473 / 437.
+bool one_wavefront(const ScoreJob& J) {
+  const int tiles = (J.classes + SCORE_TILE - 1) / SCORE_TILE;
+  return J.parts == 1 && (tiles <= 4 || (J.n_top && (tiles <= 8 || (tiles <= 32 && J.rows >= 4096))));
+}
+
 template <int TYPE, int WAVES>
 hipError_t launch_scores_waves(hipStream_t stream, const ScoreJob& J) {
   const dim3 grid(grid_of(J.rows, ST / 64 / WAVES), (unsigned)J.parts);
@@ -603,8 +613,7 @@ hipError_t launch_scores_waves(hipStream_t stream, const ScoreJob& J) {
 template <int TYPE>
 hipError_t launch_scores_type(hipStream_t stream, const ScoreJob& J) {
   if (J.classes > 64) {
-    const int tiles = (J.classes + SCORE_TILE - 1) / SCORE_TILE;
-    return tiles <= 2 ? launch_scores_waves<TYPE, 1>(stream, J) : launch_scores_waves<TYPE, 4>(stream, J);
+    return one_wavefront(J) ? launch_scores_waves<TYPE, 1>(stream, J) : launch_scores_waves<TYPE, 4>(stream, J);
   }
   CNN355_LANES(k_scores_few)
   return hipGetLastError();

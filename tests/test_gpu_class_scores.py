@@ -54,10 +54,10 @@ def _call(x, labels, top, want=("lp", "h", "norm", "top", "top_lp"), stream=None
 
 
 def _terms(rows, n):
-    """Terms that one lane adds at most."""
+    """Terms that one lane adds at most: one wavefront a row up to 8192 classes, and one more tile where a row starts oddly."""
     if n <= 64:
         return 1
-    return 16 * math.ceil(math.ceil(n / 1024) / (1 if n <= 2048 else 4))
+    return 16 * (math.ceil(math.ceil(n / 1024) / (1 if n <= 8192 else 4)) + 1)
 
 
 def _check(x, labels, top, out):
@@ -152,6 +152,19 @@ def test_ties_go_to_the_lower_index_and_order_does_not_matter(n, dtype):
     labels = torch.full((len(rows),), n - 1, dtype=torch.int32, device="cuda:0")
     for top in (1, 13, 50 if n == 50 else 64):
         _check(x, labels, top, _call(x, labels, top))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shift", [-30000.0, 500.0, 65000.0])
+@pytest.mark.parametrize("n", [12, 3000, 9000, 40000])
+def test_a_shift_of_all_classes_is_not_seen(n, shift, dtype):
+    """Large values of one sign: what is rounded is their difference."""
+    import torch
+    x, labels = _rows(4, n, "float32", n)
+    x = (x + shift).clamp(-65504, 65504).to(getattr(torch, dtype))
+    x[1, : n // 2] = shift
+    _check(x, labels, 5, _call(x, labels, 5))
+    _check_grad(x, labels, torch.ones(4, device="cuda:0"), torch.ones(4, device="cuda:0"))
 
 
 @pytest.mark.parametrize("n", [20, 3000, 50000])
