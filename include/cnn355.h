@@ -186,6 +186,15 @@ int cnn_forward_batch_scratch_bytes(cnn_t* net, size_t batch, size_t* bytes);
 int cnn_forward_batch(cnn_t* net, const float* d_images, size_t n, float* d_probs, void* d_scratch,
                       size_t scratch_bytes, size_t batch);
 
+/* A labelled set in the same pass: what cnn_class_scores (below) says of the output layer's sums, in the place of
+ * probabilities, whose logarithms are lost where they are small or close to 1.  d_log_probs [n] (minus the cross-entropy error
+ * of every image), d_entropy [n], d_top and d_top_log_probs [n][n_top], each of them or NULL; d_labels [n], 0 <= label <
+ * classes, or none (NULL if d_log_probs is).  The rest as for cnn_forward_batch, its scratch included.  CNN_E_STATE with
+ * CNN_OUTPUT_TANH_SQERR.  Asynchronous. */
+int cnn_score_batch(cnn_t* net, const float* d_images, size_t n, const int32_t* d_labels, float* d_log_probs,
+                    float* d_entropy, int n_top, int32_t* d_top, float* d_top_log_probs, void* d_scratch,
+                    size_t scratch_bytes, size_t batch);
+
 /* For callers that cannot allocate device memory (code under HIP graph capture, tight serving loops,
  * harnesses that forbid it): cnn_forward_batch with its scratch memory taken from an array inside the
  * library's device image (CNN_FORWARD_BATCH_STATIC_SCRATCH_BYTES bytes, which every GPU the library runs on
@@ -214,6 +223,14 @@ int cnn_train_step(cnn_t* net, const float* d_image, int32_t label, float lr);
  * outside the range makes the device skip that image's update and the next synchronising
  * call return CNN_E_ARG.  Asynchronous. */
 int cnn_train_many(cnn_t* net, const float* d_images, const int32_t* d_labels, size_t n, float lr);
+
+/* n train steps whose gradients are clipped: w <- w - lr f dE/dw, f = max_norm / N where the 2-norm N of all of an image's
+ * gradients is above max_norm, else 1 (cnn_clipped_update, below, on the network's own gradients and weights; a norm that is
+ * infinite or NaN leaves the weights as they are).  d_norms: [n] receives N of every image (0 where it was skipped for its
+ * label), or NULL.  Every image's gradients go through memory, so the weights cannot stay on the chip between images: two
+ * launches an image more than cnn_train_step.  max_norm >= 0, lr finite (CNN_E_ARG).  Asynchronous. */
+int cnn_train_many_clipped(cnn_t* net, const float* d_images, const int32_t* d_labels, size_t n, float lr,
+                           float max_norm, float* d_norms);
 
 /* n forward propagations; d_probs: n * cnn_num_classes floats.  Asynchronous. */
 int cnn_forward_many(cnn_t* net, const float* d_images, size_t n, float* d_probs);

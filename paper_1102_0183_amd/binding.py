@@ -86,6 +86,8 @@ def lib():
             "cnn_resident_spec_source": (C.c_int, [vp, vp, C.c_size_t]),
             "cnn_load_resident_code": (C.c_int, [vp, C.c_char_p]),
             "cnn_resident_code_active": (C.c_int, [vp]),
+            "cnn_score_batch": (C.c_int, [vp, vp, sz, vp, vp, vp, C.c_int, vp, vp, vp, sz, sz]),
+            "cnn_train_many_clipped": (C.c_int, [vp, vp, vp, sz, C.c_float, C.c_float, vp]),
             "cnn_class_scores_scratch_bytes": (C.c_int, [sz, sz, C.c_int, vp]),
             "cnn_class_scores": (C.c_int, [vp, vp, C.c_int, sz, sz, sz, vp, vp, vp, vp, C.c_int, vp, vp, vp, sz]),
             "cnn_class_scores_grad": (C.c_int, [vp, vp, C.c_int, sz, sz, sz, vp, vp, vp, vp, vp, vp, sz]),
@@ -114,7 +116,7 @@ EXPORTS = ["cnn_arch_info", "cnn_arch_info_xy", "cnn_workspace_bytes", "cnn_plan
            "cnn_set_matrix_cores", "cnn_set_launch_graph", "cnn_set_grid", "cnn_set_spin_limit", "cnn_set_barrier", "cnn_synchronize", "cnn_get_activation",
            "cnn_get_delta", "cnn_get_argmax", "cnn_get_loss", "cnn_debug_gradients", "cnn_get_stage_times", "cnn_measure_crossing", "cnn_measure_launch",
            "cnn_resident_spec_source", "cnn_load_resident_code", "cnn_resident_code_active", "cnn_debug_forward_batch_layer",
-           "cnn_deform_images", "cnn_class_scores_scratch_bytes", "cnn_class_scores", "cnn_class_scores_grad",
+           "cnn_deform_images", "cnn_score_batch", "cnn_train_many_clipped", "cnn_class_scores_scratch_bytes", "cnn_class_scores", "cnn_class_scores_grad",
            "cnn_gradient_scratch_bytes", "cnn_gradient_norm", "cnn_clip_gradients", "cnn_clipped_update", "cnn_last_error"]
 
 
@@ -584,6 +586,17 @@ class Cnn:
         self._ck(lib().cnn_train_many(self._h, d_images.data_ptr(), d_labels.data_ptr(), n, float(lr)),
                  "cnn_train_many")
 
+    def train_many_clipped(self, d_images, d_labels, lr, max_norm, d_norms=None, n=None):
+        """train_many with every image's gradients clipped to a 2-norm of max_norm; d_norms: float32 [n], their norms."""
+        torch = self._torch
+        n = d_labels.numel() if n is None else int(n)
+        assert d_labels.is_cuda and d_labels.dtype == torch.int32 and d_labels.is_contiguous()
+        assert d_labels.numel() >= n and d_images.numel() >= n * self.image_size
+        assert d_images.is_cuda and d_images.dtype == torch.float32 and d_images.is_contiguous()
+        p = None if d_norms is None else self._dev_f32(d_norms, n)
+        self._ck(lib().cnn_train_many_clipped(self._h, d_images.data_ptr(), d_labels.data_ptr(), n, float(lr), float(max_norm), p),
+                 "cnn_train_many_clipped")
+
     def forward_many(self, d_images, n, d_probs=None):
         torch = self._torch
         assert d_images.is_cuda and d_images.dtype == torch.float32 and d_images.is_contiguous()
@@ -607,6 +620,23 @@ class Cnn:
         p = self._dev_f32(d_probs, n * self.num_classes)
         self._ck(lib().cnn_forward_batch(self._h, d_images.data_ptr(), int(n), p, d_scratch.data_ptr(),
                                          d_scratch.numel(), int(batch)), "cnn_forward_batch")
+
+    def score_batch(self, d_images, n, d_scratch, batch, d_labels=None, d_log_probs=None, d_entropy=None, d_top=None, d_top_log_probs=None):
+        """forward_batch up to the output layer's sums, and class_scores of them: float32 d_log_probs [n], d_entropy [n], int32 d_top
+        and float32 d_top_log_probs [n][n_top], each or None; d_labels int32 [n]; d_scratch as for forward_batch."""
+        torch = self._torch
+        if _f32 is None:
+            _know_torch()
+        dev = d_images.device
+        assert d_images.is_cuda and d_images.dtype == torch.float32 and d_images.is_contiguous()
+        assert d_images.numel() >= n * self.image_size
+        scratch, nbytes = _scratch_of(d_scratch, dev)
+        some = d_top if d_top is not None else d_top_log_probs
+        n_top = 0 if some is None else some.shape[-1]
+        self._ck(lib().cnn_score_batch(self._h, d_images.data_ptr(), int(n), _address(d_labels, _i32, (n,), dev),
+                                       _address(d_log_probs, _f32, (n,), dev), _address(d_entropy, _f32, (n,), dev), n_top,
+                                       _address(d_top, _i32, (n, n_top), dev), _address(d_top_log_probs, _f32, (n, n_top), dev),
+                                       scratch, nbytes, int(batch)), "cnn_score_batch")
 
     def debug_forward_batch_layer(self, d_images, n, trainable_layer, d_scratch):
         """Outputs of one trainable layer of the batched forward pass for n images run as one batch: (n, floats)."""

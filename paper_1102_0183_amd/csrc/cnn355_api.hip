@@ -328,6 +328,7 @@ struct cnn {
   int graph_built_for[2] = {0, 0};
   float* d_weights = nullptr;
   float* d_grad = nullptr;
+  double* d_clip_sums = nullptr;   // sums of squares of d_grad (cnn_train_many_clipped)
   float* d_fe_filters = nullptr;
   int* d_fe_src = nullptr;
   float* d_fe_out = nullptr;
@@ -406,6 +407,7 @@ size_t carve(cnn* net, void* base) {
   net->d_call = c.take<CallArgs>(1);
   net->d_weights = c.take<float>(nw);
   net->d_grad = c.take<float>(nw);
+  net->d_clip_sums = c.take<double>(LIST_SUMS);
   net->d_fe_filters = c.take<float>((size_t)A[0].maps * MAX_FRONTEND_K * MAX_FRONTEND_K);
   net->d_fe_src = c.take<int>(A[0].maps);
   net->d_fe_out = c.take<float>((size_t)A[0].maps * A[0].h * A[0].w);
@@ -2000,7 +2002,7 @@ int over_gradients(const char* call, hipStream_t stream, const cnn_tensor* grads
   for (size_t i = 0; i < n; ++i) live += grads[i].n != 0;
   // the tensors that hold something, in the kernels' argument where they fit there, else in memory, an argument after the other
   TensorJob J;
-  J.table = nullptr; J.tensors = 0; J.chunks = 0; J.sums = 0;
+  J.table = nullptr; J.tensors = 0; J.chunks = 0; J.sums = 0; J.label = nullptr; J.classes = 0;
   hipError_t e = hipSuccess;
   bool in_place = true;
   size_t written = 0;
@@ -2924,12 +2926,14 @@ int cnn355_deform_form(int C, int H, int W, float sigma) {
 }
 
 // tap_step >= 0 (parity tap): the pass stops behind that trainable layer and its outputs for the n <= batch
-// images, [image][out_per_image], are copied to host_tap; d_probs is not written then.
+// images, [image][out_per_image], are copied to host_tap; d_probs is not written then.  scores: the pass ends with the output
+// layer's sums, and what is asked for of them (d_probs is not written either).
 static int forward_batch_impl(cnn_t* net, const float* d_images, size_t n, float* d_probs, void* d_scratch,
-                              size_t scratch_bytes, size_t batch, int tap_step, float* host_tap, size_t* tap_per_image) {
+                              size_t scratch_bytes, size_t batch, int tap_step, float* host_tap, size_t* tap_per_image,
+                              const ScoreJob* scores = nullptr) {
   if (!net) return fail(nullptr, CNN_E_ARG, "NULL handle");
   if (n == 0) return CNN_OK;
-  if (!d_images || (!d_probs && tap_step < 0) || !d_scratch || batch == 0) return fail(&net->err, CNN_E_ARG, "NULL argument or batch of 0");
+  if (!d_images || (!d_probs && tap_step < 0 && !scores) || !d_scratch || batch == 0) return fail(&net->err, CNN_E_ARG, "NULL argument or batch of 0");
   if (((uintptr_t)d_scratch & 255u) != 0) return fail(&net->err, CNN_E_ARG, "scratch must be 256-byte aligned");
   std::shared_ptr<const BatchKept> kept;
   int rc = batch_plan(net, batch, kept);
@@ -2976,6 +2980,8 @@ static int forward_batch_impl(cnn_t* net, const float* d_images, size_t n, float
       in = d_fe;
       in_stride = (long long)fe_sz;
     }
+    const int units = scores ? OUT_SUMS : net->out_units;
+    float* probs = scores ? nullptr : d_probs + t0 * P.n_classes;   // scores: the sums, in a buffer that no layer needs any more
     int cur = 0;
     bool done = false;
     const BatchPool* last_raw = nullptr;
@@ -3012,6 +3018,7 @@ static int forward_batch_impl(cnn_t* net, const float* d_images, size_t n, float
       if (raw && s + 1 == B.steps.size() && tap_step < 0 && outputs_add(P.n_classes, st.pool.n_slices)) {
         last_raw = &st.pool;
         in = d_sums;
+        if (scores) probs = d_act[cur];
         break;
       }
       const bool tail = B.tail && s + 2 == B.steps.size() && tap_step < 0;
@@ -3023,10 +3030,11 @@ static int forward_batch_impl(cnn_t* net, const float* d_images, size_t n, float
       }
       if (tail) {
         const LayerDev& L = P.layers[P.n_layers - 1];
+        if (scores) probs = d_act[cur ^ 1];
         BatchTail t;
-        t.in = add ? d_sums : out; t.bias_h = add ? st.pool.bias : nullptr; t.w = L.w; t.bias = L.bias; t.out = d_probs + t0 * P.n_classes;
+        t.in = add ? d_sums : out; t.bias_h = add ? st.pool.bias : nullptr; t.w = L.w; t.bias = L.bias; t.out = probs;
         t.n = (long long)nb; t.slice_stride = st.pool.slice_stride; t.n_slices = add ? st.pool.n_slices : 1;
-        t.n_hidden = L.n_in; t.n_out = L.n_out; t.out_units = net->out_units; t.drop = B.steps.back().raw();
+        t.n_hidden = L.n_in; t.n_out = L.n_out; t.out_units = units; t.drop = B.steps.back().raw();
         HIP_TRY(net, launch_batch_tail(net->stream, t));
         done = true;
         break;
@@ -3062,10 +3070,21 @@ static int forward_batch_impl(cnn_t* net, const float* d_images, size_t n, float
         return CNN_OK;
       }
     }
-    if (done) continue;
-    HIP_TRY(net, launch_batch_outputs(net->stream, in, last_raw ? last_raw->n_slices : 1, last_raw ? last_raw->slice_stride : 0,
-                                      last_raw ? (const float*)last_raw->bias : nullptr, d_probs + t0 * P.n_classes, (long long)nb,
-                                      P.n_classes, net->out_units));
+    // (sums that are whole already are the last layer's outputs as they lie)
+    if (!done && scores && !last_raw) probs = const_cast<float*>(in);
+    else if (!done)
+      HIP_TRY(net, launch_batch_outputs(net->stream, in, last_raw ? last_raw->n_slices : 1, last_raw ? last_raw->slice_stride : 0,
+                                        last_raw ? (const float*)last_raw->bias : nullptr, probs, (long long)nb, P.n_classes, units));
+    if (scores) {
+      ScoreJob J = *scores;
+      J.x = probs; J.rows = (long long)nb;
+      if (J.labels) J.labels += t0;
+      if (J.log_probs) J.log_probs += t0;
+      if (J.entropy) J.entropy += t0;
+      if (J.top) J.top += t0 * J.n_top;
+      if (J.top_log_probs) J.top_log_probs += t0 * J.n_top;
+      HIP_TRY(net, launch_scores(net->stream, J));
+    }
   }
   return CNN_OK;
 }
@@ -3073,6 +3092,45 @@ static int forward_batch_impl(cnn_t* net, const float* d_images, size_t n, float
 int cnn_forward_batch(cnn_t* net, const float* d_images, size_t n, float* d_probs, void* d_scratch,
                       size_t scratch_bytes, size_t batch) {
   return forward_batch_impl(net, d_images, n, d_probs, d_scratch, scratch_bytes, batch, -1, nullptr, nullptr);
+}
+
+int cnn_score_batch(cnn_t* net, const float* d_images, size_t n, const int32_t* d_labels, float* d_log_probs, float* d_entropy,
+                    int n_top, int32_t* d_top, float* d_top_log_probs, void* d_scratch, size_t scratch_bytes, size_t batch) {
+  if (!net) return fail(nullptr, CNN_E_ARG, "NULL handle");
+  if (net->out_units != CNN_OUTPUT_SOFTMAX_XENT) return fail(&net->err, CNN_E_STATE, "cnn_score_batch: the output units are not a soft-max");
+  if (n_top < 0 || n_top > SCORE_TOP || n_top > net->n_classes) return fail(&net->err, CNN_E_ARG, "cnn_score_batch: 0 to 64 best classes, no more than there are");
+  if (d_log_probs && !d_labels) return fail(&net->err, CNN_E_ARG, "cnn_score_batch: log probabilities of labels without labels");
+  if (!d_top && !d_top_log_probs) n_top = 0;
+  ScoreJob J;
+  J.x = nullptr; J.labels = d_labels; J.log_probs = d_log_probs; J.entropy = d_entropy; J.normaliser = nullptr;
+  J.top = n_top ? d_top : nullptr; J.top_log_probs = n_top ? d_top_log_probs : nullptr;
+  J.part_best = nullptr; J.part_sums = nullptr;
+  J.rows = 0; J.stride = net->n_classes; J.classes = net->n_classes; J.type = CNN_TYPE_F32; J.n_top = n_top;
+  J.parts = 1; J.part_tiles = (net->n_classes + SCORE_TILE - 1) / SCORE_TILE;
+  return forward_batch_impl(net, d_images, n, nullptr, d_scratch, scratch_bytes, batch, -1, nullptr, nullptr, &J);
+}
+
+int cnn_train_many_clipped(cnn_t* net, const float* d_images, const int32_t* d_labels, size_t n, float lr, float max_norm, float* d_norms) {
+  if (!net || !d_images || !d_labels) return fail(net ? &net->err : nullptr, CNN_E_ARG, "NULL argument");
+  if (!(max_norm >= 0.f) || !std::isfinite(lr)) return fail(&net->err, CNN_E_ARG, "cnn_train_many_clipped: max_norm is negative or NaN, or lr not finite");
+  // all weights, and all gradients, are one tensor
+  TensorJob J;
+  J.table = nullptr; J.tensors = 1; J.classes = net->n_classes;
+  J.e[0].from = net->d_grad; J.e[0].to = net->d_weights; J.e[0].n = net->n_weights; J.e[0].chunk = 0; J.e[0].type = CNN_TYPE_F32;
+  J.chunks = (unsigned)((net->n_weights * sizeof(float) + LIST_CHUNK - 1) / LIST_CHUNK);
+  J.sums = (int)std::min(J.chunks, (unsigned)LIST_SUMS);
+  for (size_t t = 0; t < n; ++t) {
+    RunArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.images = d_images + t * net->image_size; a.labels = d_labels + t; a.n_images = 1; a.image_stride = (long long)net->image_size;
+    a.train = 1; a.grad_out = net->d_grad;
+    int rc = run(net, a);
+    if (rc) return rc;
+    J.label = d_labels + t;
+    HIP_TRY(net, launch_squares(net->stream, J, net->d_clip_sums));
+    HIP_TRY(net, launch_update(net->stream, J, net->d_clip_sums, max_norm, lr, d_norms ? d_norms + t : nullptr));
+  }
+  return CNN_OK;
 }
 
 int cnn_debug_forward_batch_layer(cnn_t* net, const float* d_images, size_t n, int trainable_layer, float* host_out,

@@ -15,6 +15,7 @@
 
 #define CNN_GLOBAL __attribute__((address_space(1)))
 #include "cnn355_dev.h"
+#include "cnn355_ops.h"
 
 namespace cnn355 {
 
@@ -1471,7 +1472,7 @@ __global__ void __launch_bounds__(256) k_batch_outputs(cgf sums, int n_slices, l
       const float x = bias ? fmaxf(add_planes(a + k, n_slices, slice_stride), -INFINITY) + bias[k] : a[k];
       o[k] = out_units == 1 ? b_act(x) : x;
     }
-    if (out_units == 1) return;
+    if (out_units != 0) return;   // (OUT_SUMS: the sums as they are)
     v = o;
   }
   // (sums that are there already are read where they are: through the outputs, 1000 classes took 1.25 times as long)
@@ -1573,6 +1574,7 @@ __global__ void __launch_bounds__(256) k_batch_tail(BatchTail g) {
     }
     float out = 0.f;
     if (g.out_units == 1) out = b_act(mine);
+    else if (g.out_units == OUT_SUMS) out = mine;
     else {
       float most = mine;
       for (int d = top; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));

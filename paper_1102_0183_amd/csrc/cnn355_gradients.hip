@@ -248,6 +248,10 @@ __global__ void __launch_bounds__(GT) k_scale(TensorJob J, const CNN_GLOBAL doub
 template <bool FAR>
 __global__ void __launch_bounds__(GT) k_update(TensorJob J, const CNN_GLOBAL double* sums, double max_norm, double lr, CNN_GLOBAL float* norm) {
   __shared__ double lds[GT / 64];
+  if (J.label && (J.label[0] < 0 || J.label[0] >= J.classes)) {
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = 0.0f;
+    return;
+  }
   const double v = norm_of(sums, J.sums, lds);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
   if (!(v < __builtin_inf())) return;

@@ -13,6 +13,8 @@ namespace cnn355 {
 enum ElementType : int { ELEMENT_F32 = 0, ELEMENT_BF16 = 1, ELEMENT_F16 = 2 };   // CNN_TYPE_* of the C ABI
 constexpr size_t element_bytes(int type) { return type == ELEMENT_F32 ? 4 : 2; }
 
+constexpr int OUT_SUMS = 2;   // batched forward pass, in the place of CNN_OUTPUT_*: the output layer's sums, without units
+
 // ---- scores of classes ------------------------------------------------------------------------
 constexpr int SCORE_TOP = 64;      // best classes at most: one a lane
 constexpr int SCORE_TILE = 1024;   // classes that a wavefront looks at together, 16 a lane
@@ -62,6 +64,8 @@ struct TensorJob {
   int tensors;
   unsigned int chunks;             // of all tensors
   int sums;                        // workgroups that leave a sum
+  const CNN_GLOBAL int* label;     // null, or of the image that the gradients are of: outside [0, classes) it is passed over
+  int classes;
   TensorEntry e[LIST_MOST];
 };
 
