@@ -436,7 +436,8 @@ int cnn_deform_images(void* hip_stream, const float* d_src, size_t n_src, float*
  *     (from cnn_class_scores) with the second.  d_grad may be d_logits with the same stride; otherwise what lies
  *     between the first and the last element of one must not overlap the other.  What lies between the rows is
  *     left as it is.  (The error -log p_label averaged over n rows: g_l = -1/n.)
- * Sums are fp32 for every type.  hip_stream: a hipStream_t (NULL: the default stream) of the current device.
+ * Sums are fp32 for every type; the same call gives the same bits, and its last ones may depend on how many rows there are and
+ * which outputs are asked for.  hip_stream: a hipStream_t (NULL: the default stream) of the current device.
  * Asynchronous; nothing is allocated.  rows up to 2^31 - 1, classes up to 2^30; rows == 0 does nothing.
  * Errors: CNN_E_ARG, CNN_E_SHAPE, CNN_E_WORKSPACE, CNN_E_HIP; the message is cnn_last_error(NULL)'s. */
 enum { CNN_TYPE_F32 = 0, CNN_TYPE_BF16 = 1, CNN_TYPE_F16 = 2 };

@@ -62,7 +62,7 @@ hipError_t launch_batch_outputs(hipStream_t stream, const float* sums, int n_sli
 hipError_t launch_batch_pack(hipStream_t stream, const BatchPackAll& all);
 hipError_t launch_deform(hipStream_t stream, const DeformJob& J);
 bool deform_mx_is_faster(const DeformJob& J);
-void score_parts(long long rows, int classes, int* parts, int* part_tiles);
+void score_parts(long long rows, int classes, int n_top, int* parts, int* part_tiles);
 hipError_t launch_scores(hipStream_t stream, const ScoreJob& J);
 hipError_t launch_scores_grad(hipStream_t stream, const ScoreGradJob& J);
 hipError_t launch_table(hipStream_t stream, const TensorJob& J, TensorEntry* at);
@@ -2825,7 +2825,7 @@ static int check_rows(const char* call, int type, size_t rows, size_t classes, s
 }
 
 static size_t score_scratch(size_t rows, size_t classes, int n_top, int* parts, int* part_tiles) {
-  score_parts((long long)rows, (int)classes, parts, part_tiles);
+  score_parts((long long)rows, (int)classes, n_top, parts, part_tiles);
   return *parts == 1 ? 0 : rows * *parts * (16 + 8 * (size_t)n_top);
 }
 

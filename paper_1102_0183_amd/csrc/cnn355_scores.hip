@@ -82,52 +82,57 @@ __device__ __forceinline__ void for_distances(F f) {
   if constexpr (LANES > 32) f(std::integral_constant<int, 32>());
 }
 
-// Bitonic sorting: groups of LANES lanes that rise and then fall, or the other way round, in falling order, every second one
-// in rising order.
-template <int LANES, int D, class T>
-__device__ __forceinline__ T merge_steps(T v) {
+// a lane's value and that of lane ^ D, in either order
+template <int D, class T>
+__device__ __forceinline__ void pair_of(T v, T& a, T& b) {
+  if constexpr (D < 16) {
+    a = v;
+    b = xor_lane<D>(v);
+  } else {   // (the swap leaves both halves' values in every lane)
+    unsigned w[2 * sizeof(T) / 4];
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(T) / 4; ++i) {
+      unsigned x;
+      if constexpr (sizeof(T) == 8) x = i ? (unsigned)(v >> 32) : (unsigned)v;
+      else x = __builtin_bit_cast(unsigned, v);
+      const auto r = D == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+      w[i] = r[0];
+      w[sizeof(T) / 4 + i] = r[1];
+    }
+    if constexpr (sizeof(T) == 8) {
+      a = (u64)w[1] << 32 | w[0];
+      b = (u64)w[3] << 32 | w[2];
+    } else {
+      a = __builtin_bit_cast(T, w[0]);
+      b = __builtin_bit_cast(T, w[1]);
+    }
+  }
+}
+
+// Bitonic sorting: lanes that rise and then fall, or the other way round, in groups of 2 D to fall, or to rise where
+// (lane & RISE) != 0 (64: in all of them, 0: in none).
+template <int D, int RISE, class T>
+__device__ __forceinline__ T merge_lanes(T v) {
   if constexpr (D >= 1) {
     const int lane = threadIdx.x & 63;
-    const T o = xor_lane<D>(v);
-    const bool want_larger = ((lane & D) == 0) == ((lane & LANES) == 0);
-    v = (v < o) == want_larger ? o : v;   // (equal ones: either)
-    return merge_steps<LANES, D / 2>(v);
+    const bool rises = RISE == 64 || (lane & RISE) != 0, larger = ((lane & D) == 0) != rises;
+    T a, b;
+    pair_of<D>(v, a, b);
+    v = (a < b) == larger ? b : a;   // (equal ones: either)
+    return merge_lanes<D / 2, RISE>(v);
   } else {
     return v;
   }
 }
-// ... of any groups
-template <int LANES, class T>
-__device__ __forceinline__ T sort_steps(T v) {
-  if constexpr (LANES > 2) v = sort_steps<LANES / 2>(v);
-  return merge_steps<LANES, LANES / 2>(v);
-}
-// ... all of them in falling order
-template <int D, class T>
-__device__ __forceinline__ T fall_steps(T v) {
-  if constexpr (D >= 1) {
-    const T o = xor_lane<D>(v);
-    v = (v < o) == ((threadIdx.x & D) == 0) ? o : v;
-    return fall_steps<D / 2>(v);
-  } else {
-    return v;
-  }
-}
-// every group of LANES lanes in falling order
-template <int LANES, class T>
+// every group of LANES lanes in falling order; RISE as above
+template <int LANES, int RISE, class T>
 __device__ __forceinline__ T sort_lanes(T v) {
-  if constexpr (LANES > 2) v = sort_steps<LANES / 2>(v);
-  return fall_steps<LANES / 2>(v);
+  if constexpr (LANES > 2) v = sort_lanes<LANES / 2, LANES / 2>(v);
+  return merge_lanes<LANES / 2, RISE>(v);
 }
-// the larger ones of two sorted runs of 64, sorted: the second one comes in rising order
-template <class T>
-__device__ __forceinline__ T best_of(T falling, T rising) { return fall_steps<32>(falling < rising ? rising : falling); }
-// sorted the other way round
-template <class T>
-__device__ __forceinline__ T reversed(T v) {
-  for_distances<64>([&](auto d) { v = xor_lane<decltype(d)::value>(v); });
-  return v;
-}
+// the larger ones of two sorted runs of 64, the first falling and the second rising; sorted
+template <int RISE, class T>
+__device__ __forceinline__ T best_of(T falling, T rising) { return merge_lanes<32, RISE>(falling < rising ? rising : falling); }
 
 // ---- sums of a row ----
 struct Sums {
@@ -171,18 +176,44 @@ __device__ __forceinline__ Row row_of(const Sums& a) {
 }
 __device__ __forceinline__ float log_prob(const Row& r, float x) { return r.m == -INFINITY ? -INFINITY : (x - r.m) - r.log_s; }
 
-// One lane's share of a row's results: lane 0 the numbers, lane i the i-th of the best.
+// A row's label and its value, asked for before the row is looked at (two loads one after the other).
+struct Label {
+  bool is;
+  float x;
+};
 template <int TYPE>
-__device__ __forceinline__ void give_row(const ScoreJob& J, long long row, int lane, const Sums& a, u64 best) {
+__device__ __forceinline__ Label label_of(const ScoreJob& J, long long row) {
   typedef Element<TYPE> E;
+  Label l = {false, 0.0f};
+  if (J.log_probs) {
+    const int c = J.labels[row];
+    l.is = c >= 0 && c < J.classes;
+    if (l.is) l.x = E::get(((const CNN_GLOBAL typename E::T*)J.x)[row * J.stride + c]);
+  }
+  return l;
+}
+
+// Where fewer classes than are asked for are above -inf, the masked ones with the lowest indices follow: fewer than 64 are not
+// masked, so of the first 128 there are enough that are.
+template <int TYPE>
+__device__ __forceinline__ u64 with_masked(const ScoreJob& J, long long row, u64 list) {
+  typedef Element<TYPE> E;
+  const int lane = threadIdx.x & 63;
+  int have = __popcll(__ballot(list != 0));
+  for (int first = 0; first < 128 && have < J.n_top; first += 64) {
+    const int c = first + lane;
+    const bool is = c < J.classes && E::get(((const CNN_GLOBAL typename E::T*)J.x)[row * J.stride + min(c, J.classes - 1)]) == -INFINITY;
+    for (u64 in = __ballot(is); in && have < J.n_top; in &= in - 1, ++have)
+      if (lane == have) list = key_of(-INFINITY, first + __builtin_ctzll(in));
+  }
+  return list;
+}
+
+// One lane's share of a row's results: lane 0 the numbers, lane i the i-th of the best.
+__device__ __forceinline__ void give_row(const ScoreJob& J, long long row, int lane, const Sums& a, const Label& l, u64 best) {
   const Row r = row_of(a);
   if (lane == 0) {
-    if (J.log_probs) {
-      const int l = J.labels[row];
-      float v = 0.0f;
-      if (l >= 0 && l < J.classes) v = log_prob(r, E::get(((const CNN_GLOBAL typename E::T*)J.x)[row * J.stride + l]));
-      J.log_probs[row] = v;
-    }
+    if (J.log_probs) J.log_probs[row] = l.is ? log_prob(r, l.x) : 0.0f;
     if (J.entropy) J.entropy[row] = r.entropy;
     if (J.normaliser) { J.normaliser[2 * row] = r.m; J.normaliser[2 * row + 1] = r.log_s; }
   }
@@ -203,7 +234,7 @@ struct Picking {             // LDS of a wavefront
 };
 
 struct Best {
-  u64 list;        // lane i: the i-th best so far, 0: none
+  u64 list;        // lane i: the i-th best so far, 0: none (masked classes, -inf, are none)
   u64 bar;         // a key that can still be among them is above it,
   float bar_value; // and the value of a class of the next tile that can is not below this
   int held;
@@ -226,7 +257,7 @@ __device__ __forceinline__ void take_held(Best& b, Picking& L, int n_top) {
   lds_order();
   L.held[lane] = rest;
   b.held = b.held > 64 ? b.held - 64 : 0;
-  b.list = best_of(b.list, reversed(sort_lanes<64>(mine)));
+  b.list = best_of<0>(b.list, sort_lanes<64, 64>(mine));
   const u64 last = lane_of(b.list, n_top - 1);
   if (last > b.bar) {
     // (the classes of the tiles to come have higher indices: of theirs, only larger values are above that key)
@@ -255,20 +286,21 @@ __device__ __forceinline__ RowAt<TYPE> row_at(const ScoreJob& J, long long row) 
 //
 // As many classes as are asked for reach the n_top-th of the lanes' largest values, so what lies below it is out.  Of G such
 // values and n_top best G log(G / (G - n_top)) classes reach it where their order is chance: 24 of 64 for 20, 89 of 128 for 64
-// (and 300 of 64).  Their classes are asked for again, one to a lane, 16 lanes' at a time.
+// (and 300 of 64).  Their classes are asked for again, one to a lane, 32 lanes' at a time.
 // (Looking at every tile as it comes, against the best so far, finds some in every second tile of a row of 131072: 4096 such
 // rows with 20 best took 252 us so, 194 without any best.)
 template <int TYPE>
-__device__ __forceinline__ void pick(Best& b, Picking& L, const RowAt<TYPE>& row, float m0, float m1, int first, int step, int tiles, int n_top) {
+__device__ __forceinline__ void pick(Best& b, Picking& L, const RowAt<TYPE>& row, float m0, float m1, int first, int step, int tiles, bool last, int n_top) {
   typedef Element<TYPE> E;
   constexpr int V = E::V;
   const int lane = threadIdx.x & 63;
-  const float v = lane_of(n_top <= 24 ? sort_lanes<64>(fmaxf(m0, m1)) : best_of(sort_lanes<64>(m0), reversed(sort_lanes<64>(m1))), n_top - 1);
-  if (v > LOWEST && v > b.bar_value) {   // (LOWEST: lanes without any)
+  const float v = lane_of(n_top <= 24 ? sort_lanes<64, 0>(fmaxf(m0, m1)) : best_of<0>(sort_lanes<64, 0>(m0), sort_lanes<64, 64>(m1)), n_top - 1);
+  if (v > b.bar_value) {
     b.bar_value = v;
     b.bar = key_of(v, -1);
   }
   int waiting = 0;
+#pragma unroll 1
   for (int i = 0; i < tiles; ++i) {
     const u64 in = __ballot(__builtin_bit_cast(float, (unsigned)L.largest[i][lane] << 16) >= b.bar_value);
     if (in) {
@@ -277,23 +309,27 @@ __device__ __forceinline__ void pick(Best& b, Picking& L, const RowAt<TYPE>& row
     }
     if (waiting < 64 && i + 1 < tiles) continue;
     lds_order();
-    for (int w0 = 0; w0 < waiting; w0 += 16) {
-      u64 key[4];
+    const bool finish = last && i + 1 == tiles;   // (what is held joins the list here too: its code is there once)
+#pragma unroll 1
+    for (int w0 = 0; w0 < waiting || (finish && w0 == 0); w0 += 32) {
+      u64 key[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < 8; ++u) {
         const int w = w0 + u * 4 + (lane >> 4), k = lane & 15;
         const int at_lane = w < waiting ? L.where[w] : 0;
         const int at = (first + (at_lane >> 6) * step) * SCORE_TILE + (k / V) * 64 * V + (at_lane & 63) * V + k % V;
         key[u] = w < waiting && at >= row.lead && at < row.end ? key_of_any(E::get(row.at[at]), at - row.lead) : 0;
       }
 #pragma unroll 1
-      for (int u = 0; u < 4; ++u) {
-        const u64 k = u == 0 ? key[0] : u == 1 ? key[1] : u == 2 ? key[2] : key[3];
-        const u64 take = __ballot(k > b.bar);
-        if (!take) continue;
+      for (int u = 0; u < 8; ++u) {
+        const u64 k = key[0], take = __ballot(k > b.bar);
+#pragma unroll
+        for (int j = 0; j < 7; ++j) key[j] = key[j + 1];
         if (k > b.bar) L.held[b.held + place_in(take)] = k;
         b.held += __popcll(take);
-        if (b.held >= 64) take_held(b, L, n_top);
+        const bool end = w0 + (u + 1) * 4 >= waiting;
+        while (b.held >= 64 || (end && finish && b.held)) take_held(b, L, n_top);
+        if (end) break;
       }
     }
     waiting = 0;
@@ -328,7 +364,7 @@ __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step
   typedef Element<TYPE> E;
   constexpr int V = E::V, N = 16 / V;
   a = Sums{LOWEST, 0.0f, 0.0f};
-  b = Best{0, 0, -INFINITY, 0};
+  b = Best{0, key_of(-INFINITY, 0), LOWEST, 0};
   float r = -INFINITY;
   float largest[2] = {LOWEST, LOWEST};
   bool rough = false;
@@ -388,13 +424,12 @@ __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step
       const unsigned bits = __builtin_bit_cast(unsigned, max3(top[0], top[1], top[1]));
       L->largest[in_segment++][threadIdx.x & 63] = (unsigned short)((TYPE == ELEMENT_BF16 || (int)bits < 0 ? bits : bits + 0xffffu) >> 16);
       if (in_segment == SEGMENT || tile + step >= last) {
-        pick<TYPE>(b, *L, row, largest[0], largest[1], tile - (in_segment - 1) * step, step, in_segment, n_top);
+        pick<TYPE>(b, *L, row, largest[0], largest[1], tile - (in_segment - 1) * step, step, in_segment, tile + step >= last, n_top);
         in_segment = 0;
       }
     }
   }
   if (!rough) settle();
-  if (TOP && b.held) take_held(b, *L, n_top);
 }
 
 // Rows of more than 64 classes, WAVES wavefronts a row or, where parts > 1, a part of one.
@@ -410,6 +445,8 @@ __global__ void __launch_bounds__(ST) k_scores(ScoreJob J) {
   for (long long row = (long long)blockIdx.x * ROWS + part_of; row < J.rows; row += (long long)gridDim.x * ROWS) {
     Sums a;
     Best b;
+    Label label = {false, 0.0f};
+    if (J.parts == 1 && w == 0) label = label_of<TYPE>(J, row);
     const RowAt<TYPE> x = row_at<TYPE>(J, row);
     const int tiles = (x.end + SCORE_TILE - 1) / SCORE_TILE;   // (one more than the parts were planned for, it may be)
     scan<TYPE, ENTROPY, TOP>(x, part * J.part_tiles + w, WAVES, part + 1 == J.parts ? tiles : (part + 1) * J.part_tiles, J.n_top, a, b,
@@ -424,8 +461,10 @@ __global__ void __launch_bounds__(ST) k_scores(ScoreJob J) {
       a = Sums{LOWEST, 0.0f, 0.0f};
       if (lane < WAVES) a = Sums{lds_sums[lane][0], lds_sums[lane][1], lds_sums[lane][2]};
       join_lanes<64>(a);
-      if (TOP)
-        for (int o = 1; o < WAVES; ++o) b.list = best_of(b.list, lds_best[o][63 - lane]);
+      if (TOP) {
+#pragma unroll 1
+        for (int o = 1; o < WAVES; ++o) b.list = best_of<0>(b.list, lds_best[o][63 - lane]);
+      }
     }
     if (J.parts > 1) {
       const long long at = row * J.parts + part;
@@ -436,17 +475,21 @@ __global__ void __launch_bounds__(ST) k_scores(ScoreJob J) {
       if (TOP && lane < J.n_top) J.part_best[at * J.n_top + lane] = b.list;
       continue;
     }
-    give_row<TYPE>(J, row, lane, a, b.list);
+    if (TOP) b.list = with_masked<TYPE>(J, row, b.list);
+    give_row(J, row, lane, a, label, b.list);
   }
 }
 
 // The parts of rows joined: a workgroup a row.
+constexpr int JOINED = 8;   // lists that a wavefront asks for together (one after the other, 32 of them took it 5 us)
 template <int TYPE>
 __global__ void __launch_bounds__(ST) k_scores_join(ScoreJob J) {
   __shared__ u64 lds_best[ST / 64][64];
   __shared__ float lds_sums[ST / 64][4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (long long row = blockIdx.x; row < J.rows; row += gridDim.x) {
+    Label label = {false, 0.0f};
+    if (wave == 0) label = label_of<TYPE>(J, row);
     Sums a{LOWEST, 0.0f, 0.0f};
     if ((int)threadIdx.x < J.parts) {
       const CNN_GLOBAL float* p = J.part_sums + (row * J.parts + threadIdx.x) * 4;
@@ -455,9 +498,20 @@ __global__ void __launch_bounds__(ST) k_scores_join(ScoreJob J) {
     join_lanes<64>(a);
     u64 list = 0;
     if (J.n_top)
-      for (int part = wave; part < J.parts; part += ST / 64) {
-        const u64 k = 63 - lane < J.n_top ? J.part_best[(row * J.parts + part) * J.n_top + 63 - lane] : 0;
-        list = best_of(list, k);
+      for (int p0 = wave; p0 < J.parts; p0 += JOINED * ST / 64) {
+        u64 k[JOINED];
+#pragma unroll
+        for (int u = 0; u < JOINED; ++u) {
+          const int part = p0 + u * (ST / 64);
+          k[u] = part < J.parts && 63 - lane < J.n_top ? J.part_best[(row * J.parts + part) * J.n_top + 63 - lane] : 0;
+        }
+        // (a loop: code that runs once a launch waits for its instructions more than for what they do)
+#pragma unroll 1
+        for (int u = 0; u < JOINED && p0 + u * (ST / 64) < J.parts; ++u) {
+          list = best_of<0>(list, k[0]);
+#pragma unroll
+          for (int i = 0; i + 1 < JOINED; ++i) k[i] = k[i + 1];
+        }
       }
     __syncthreads();
     if (lane == 0) { lds_sums[wave][0] = a.m; lds_sums[wave][1] = a.s; lds_sums[wave][2] = a.t; }
@@ -467,9 +521,12 @@ __global__ void __launch_bounds__(ST) k_scores_join(ScoreJob J) {
     a = Sums{LOWEST, 0.0f, 0.0f};
     if (lane < ST / 64) a = Sums{lds_sums[lane][0], lds_sums[lane][1], lds_sums[lane][2]};
     join_lanes<64>(a);
-    if (J.n_top)
-      for (int o = 1; o < ST / 64; ++o) list = best_of(list, lds_best[o][63 - lane]);
-    give_row<TYPE>(J, row, lane, a, list);
+    if (J.n_top) {
+#pragma unroll 1
+      for (int o = 1; o < ST / 64; ++o) list = best_of<0>(list, lds_best[o][63 - lane]);
+    }
+    if (J.n_top) list = with_masked<TYPE>(J, row, list);
+    give_row(J, row, lane, a, label, list);
   }
 }
 
@@ -481,6 +538,7 @@ __global__ void __launch_bounds__(ST) k_scores_few(ScoreJob J) {
   const long long all = (J.rows + ST / L - 1) / (ST / L) * (ST / L);   // (lanes of a wavefront stay together)
   for (long long row = (long long)blockIdx.x * (ST / L) + threadIdx.x / L; row < all; row += (long long)gridDim.x * (ST / L)) {
     const bool is = row < J.rows && c < J.classes;
+    const int l = row < J.rows && J.log_probs ? J.labels[row] : -1;
     const float x = is ? E::get(((const CNN_GLOBAL typename E::T*)J.x)[row * J.stride + c]) : -INFINITY;
     float m = fmaxf(x, LOWEST);
     for_distances<L>([&](auto d) { m = fmaxf(m, xor_lane<decltype(d)::value>(m)); });
@@ -491,8 +549,10 @@ __global__ void __launch_bounds__(ST) k_scores_few(ScoreJob J) {
       a.t += xor_lane<decltype(o)::value>(a.t);
     });
     u64 k = is ? key_of_any(x, c) : 0;
-    if (J.n_top) k = sort_lanes<L>(k);
-    if (row < J.rows) give_row<TYPE>(J, row, c, a, k);
+    if (J.n_top) k = sort_lanes<L, 0>(k);
+    Label label = {l >= 0 && l < J.classes, 0.0f};
+    label.x = __shfl(x, ((int)threadIdx.x & ~(L - 1) & 63) + (label.is ? l : 0));
+    if (row < J.rows) give_row(J, row, c, a, label, k);
   }
 }
 
@@ -632,13 +692,16 @@ hipError_t launch_scores_grad_type(hipStream_t stream, const ScoreGradJob& J) {
 
 }  // namespace
 
-// How rows are shared: parts of whole rounds of a workgroup's tiles where the rows alone do not fill the chip.
-void score_parts(long long rows, int classes, int* parts, int* part_tiles) {
+// How rows are shared where there are too few of them to fill the chip: parts of eight tiles or more, for two workgroups a compute
+// unit at most; they cost a second launch that waits for the first.  us in parts / by one workgroup a row, 20 best of bf16: one row
+// of 16384 classes 13.7 / 9.8, 32768 13.3 / 12.1, 50000 13.7 / 15.4; 300 rows of 32768 17.9 / 14.9.  Without best one row of 50000
+// takes 13.6 / 9.1, one of 97000 13.5 / 13.0.  Parts of four tiles: one row of 8192 12.5 (one workgroup 10.8), 64 of 131072 17.3 (eight 16.9).
+void score_parts(long long rows, int classes, int n_top, int* parts, int* part_tiles) {
   const int tiles = (classes + SCORE_TILE - 1) / SCORE_TILE;
   *parts = 1;
   *part_tiles = tiles;
-  if (rows >= 512 || tiles <= 4) return;
-  const long long want = std::min<long long>({(512 + rows - 1) / rows, (tiles + 3) / 4, SCORE_PARTS});
+  if (rows >= 512 || tiles <= (n_top ? 40 : 80)) return;
+  const long long want = std::min<long long>({(512 + rows - 1) / rows, (tiles + 7) / 8, SCORE_PARTS});
   *part_tiles = (int)((tiles + want * 4 - 1) / (want * 4)) * 4;
   *parts = (tiles + *part_tiles - 1) / *part_tiles;
 }

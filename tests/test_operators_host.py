@@ -54,12 +54,13 @@ def test_scratch_of_scores():
     assert binding.class_scores_scratch_bytes(10000, 10, 10) == 0
     assert binding.class_scores_scratch_bytes(1, 4096, 64) == 0
     assert binding.class_scores_scratch_bytes(512, 200000, 64) == 0
-    assert binding.class_scores_scratch_bytes(1, 131072, 20) == 32 * (16 + 8 * 20)
+    assert binding.class_scores_scratch_bytes(1, 131072, 20) == 16 * (16 + 8 * 20)
     for rows in (1, 2, 37, 511):
-        for classes in (4097, 5000, 8193, 100003, 1 << 30):
+        for classes in (4097, 50000, 65537, 100003, 1 << 30):
             n = binding.class_scores_scratch_bytes(rows, classes, 5)
             parts, odd = divmod(n, rows * (16 + 8 * 5))
             assert odd == 0 and parts <= 256, (rows, classes)
+            assert binding.class_scores_scratch_bytes(rows, classes, 0) <= n     # enough with fewer best, too
     for bad in ((1, 10, 11), (1, 100, 65), (1, 0, 0), (1, 10, -1)):
         with pytest.raises(binding.CnnError):
             binding.class_scores_scratch_bytes(*bad)
