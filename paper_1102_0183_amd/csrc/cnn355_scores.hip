@@ -209,14 +209,19 @@ __device__ __forceinline__ u64 with_masked(const ScoreJob& J, long long row, u64
   return list;
 }
 
-// One lane's share of a row's results: lane 0 the numbers, lane i the i-th of the best.
-__device__ __forceinline__ void give_row(const ScoreJob& J, long long row, int lane, const Sums& a, const Label& l, u64 best) {
+// One lane's share of a row's results: the numbers from one of them,
+__device__ __forceinline__ Row give_sums(const ScoreJob& J, long long row, bool gives, const Sums& a, const Label& l) {
   const Row r = row_of(a);
-  if (lane == 0) {
+  if (gives) {
     if (J.log_probs) J.log_probs[row] = l.is ? log_prob(r, l.x) : 0.0f;
     if (J.entropy) J.entropy[row] = r.entropy;
     if (J.normaliser) { J.normaliser[2 * row] = r.m; J.normaliser[2 * row + 1] = r.log_s; }
   }
+  return r;
+}
+// and lane i the i-th of the best.
+__device__ __forceinline__ void give_row(const ScoreJob& J, long long row, int lane, const Sums& a, const Label& l, u64 best) {
+  const Row r = give_sums(J, row, lane == 0, a, l);
   if (lane < J.n_top) {
     if (J.top) J.top[row * J.n_top + lane] = r.none ? -1 : index_of(best);
     if (J.top_log_probs) J.top_log_probs[row * J.n_top + lane] = r.none ? r.m : log_prob(r, value_of(best));
@@ -530,7 +535,7 @@ __global__ void __launch_bounds__(ST) k_scores_join(ScoreJob J) {
   }
 }
 
-// Rows of at most 64 classes: a lane a class, 64 / L rows a wavefront.
+// Rows of at most L classes, L = 16, 32 or 64: a lane a class, 64 / L rows a wavefront.
 template <int TYPE, int L>
 __global__ void __launch_bounds__(ST) k_scores_few(ScoreJob J) {
   typedef Element<TYPE> E;
@@ -553,6 +558,66 @@ __global__ void __launch_bounds__(ST) k_scores_few(ScoreJob J) {
     Label label = {l >= 0 && l < J.classes, 0.0f};
     label.x = __shfl(x, ((int)threadIdx.x & ~(L - 1) & 63) + (label.is ? l : 0));
     if (row < J.rows) give_row(J, row, c, a, label, k);
+  }
+}
+
+// Rows of up to 16 L classes: L lanes a row, 16 classes a lane, place (k / V) L V + l V + k % V lane l's k-th.  The best come one
+// by one: the largest value left, its lowest place, which then is no number.
+template <int TYPE, int L>
+__global__ void __launch_bounds__(ST) k_scores_rows(ScoreJob J) {
+  typedef Element<TYPE> E;
+  typedef typename E::T T;
+  constexpr int V = E::V, N = 16 / V;
+  const int l = threadIdx.x & (L - 1);
+  const long long all = (J.rows + ST / L - 1) / (ST / L) * (ST / L);   // (lanes of a wavefront stay together)
+  for (long long row = (long long)blockIdx.x * (ST / L) + threadIdx.x / L; row < all; row += (long long)gridDim.x * (ST / L)) {
+    const bool is = row < J.rows;
+    Label label = {false, 0.0f};
+    if (is && l == 0) label = label_of<TYPE>(J, row);
+    const CNN_GLOBAL T* from = (const CNN_GLOBAL T*)J.x + (is ? row : 0) * J.stride;
+    v4u r[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) r[q] = load16<TYPE>(from, (q * L + l) * V, is ? J.classes : 0);
+    float x[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) x[k] = E::get(r[k / V], k % V);
+    Sums a{LOWEST, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < 16; k += 2) a.m = max3(a.m, x[k], x[k + 1]);
+    for_distances<L>([&](auto d) { a.m = fmaxf(a.m, xor_lane<decltype(d)::value>(a.m)); });
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const float d = (x[k] - a.m) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+      a.s += e;
+      a.t = fmaf(e, fmaxf(d, FAR), a.t);
+    }
+    for_distances<L>([&](auto d) {
+      a.s += xor_lane<decltype(d)::value>(a.s);
+      a.t += xor_lane<decltype(d)::value>(a.t);
+    });
+    const Row sums = give_sums(J, row, is && l == 0, a, label);
+    if (!J.n_top) continue;
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if ((k / V) * L * V + l * V + k % V >= J.classes) x[k] = __builtin_nanf("");
+#pragma unroll 1
+    for (int i = 0; i < J.n_top; ++i) {
+      float best = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 16; k += 2) best = max3(best, x[k], x[k + 1]);
+      for_distances<L>([&](auto d) { best = fmaxf(best, xor_lane<decltype(d)::value>(best)); });
+      int at = 0x7fffffff;
+#pragma unroll
+      for (int k = 15; k >= 0; --k) at = x[k] == best ? (k / V) * L * V + k % V : at;
+      at = at == 0x7fffffff ? at : at + l * V;
+      for_distances<L>([&](auto d) { at = min(at, (int)xor_word<decltype(d)::value>((unsigned)at)); });
+#pragma unroll
+      for (int k = 0; k < 16; ++k) x[k] = at - l * V == (k / V) * L * V + k % V ? __builtin_nanf("") : x[k];
+      if (is && l == 0) {
+        if (J.top) J.top[row * J.n_top + i] = sums.none ? -1 : at;
+        if (J.top_log_probs) J.top_log_probs[row * J.n_top + i] = sums.none ? sums.m : log_prob(sums, best);
+      }
+    }
   }
 }
 
@@ -583,58 +648,79 @@ __device__ __forceinline__ float grad_of(const GradRow& r, float x, int c) {
   return r.empty ? 0.0f : g;
 }
 
-template <int TYPE, int L>
-__global__ void __launch_bounds__(ST) k_scores_grad_few(ScoreGradJob J) {
+// of 16 bytes, places c .. of g, which begins with class `first` and ends before place `end`
+template <int TYPE>
+__device__ __forceinline__ void put_gradients(const GradRow& r, v4u in, CNN_GLOBAL typename Element<TYPE>::T* g, int c, int end, int first) {
   typedef Element<TYPE> E;
-  const int c = threadIdx.x & (L - 1);
-  if (c >= J.classes) return;
-  for (long long row = (long long)blockIdx.x * (ST / L) + threadIdx.x / L; row < J.rows; row += (long long)gridDim.x * (ST / L)) {
-    const GradRow r = grad_row(J, row);
-    const float x = E::get(((const CNN_GLOBAL typename E::T*)J.x)[row * J.stride + c]);
-    ((CNN_GLOBAL typename E::T*)J.grad)[row * J.grad_stride + c] = E::make(grad_of(r, x, c));
+  typename E::T e[E::V];
+  v4u v = {0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < E::V; ++j) {
+    e[j] = E::make(grad_of(r, E::get(in, j), first + c + j));
+    E::put(v, j, e[j]);
+  }
+  if (c + E::V <= end) *(CNN_GLOBAL v4u_any*)(g + c) = v;
+  else {
+#pragma unroll
+    for (int j = 0; j < E::V; ++j)
+      if (c + j < end) g[c + j] = e[j];
   }
 }
 
-// a wavefront a tile
+// L lanes a row of up to 16 L classes, as k_scores_rows
+template <int TYPE, int L>
+__global__ void __launch_bounds__(ST) k_scores_grad_rows(ScoreGradJob J) {
+  typedef Element<TYPE> E;
+  typedef typename E::T T;
+  constexpr int V = E::V, N = 16 / V;
+  const int l = threadIdx.x & (L - 1);
+  for (long long row = (long long)blockIdx.x * (ST / L) + threadIdx.x / L; row < J.rows; row += (long long)gridDim.x * (ST / L)) {
+    const CNN_GLOBAL T* x = (const CNN_GLOBAL T*)J.x + row * J.stride;
+    CNN_GLOBAL T* g = (CNN_GLOBAL T*)J.grad + row * J.grad_stride;
+    v4u in[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) in[q] = load16<TYPE>(x, (q * L + l) * V, J.classes);
+    const GradRow r = grad_row(J, row);
+#pragma unroll
+    for (int q = 0; q < N; ++q) put_gradients<TYPE>(r, in[q], g, (q * L + l) * V, J.classes, 0);
+  }
+}
+
+// A wavefront a tile of its workgroup's four, row after row, gridDim.y apart, the next one's values under way.  (Rows that start
+// at odd addresses take 4 % longer, tiles that begin with 16 whole bytes or not.)
 template <int TYPE>
 __global__ void __launch_bounds__(ST) k_scores_grad(ScoreGradJob J) {
   typedef Element<TYPE> E;
   typedef typename E::T T;
   constexpr int V = E::V, N = 16 / V;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tiles = (J.classes + SCORE_TILE - 1) / SCORE_TILE;
-  const long long n = J.rows * tiles;
-  for (long long at = (long long)blockIdx.x * (ST / 64) + wave; at < n; at += (long long)gridDim.x * (ST / 64)) {
-    const long long row = at / tiles;
-    const int first = (int)(at - row * tiles) * SCORE_TILE;
-    const CNN_GLOBAL T* x = (const CNN_GLOBAL T*)J.x + row * J.stride;
-    CNN_GLOBAL T* g = (CNN_GLOBAL T*)J.grad + row * J.grad_stride;
+  const int first = (blockIdx.x * (ST / 64) + wave) * SCORE_TILE, end = J.classes - first;
+  if (end <= 0) return;
+  const CNN_GLOBAL T* x = (const CNN_GLOBAL T*)J.x + first;
+  CNN_GLOBAL T* g = (CNN_GLOBAL T*)J.grad + first;
+  v4u next[N];
+  auto load = [&](long long row) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) next[q] = load16<TYPE>(x + row * J.stride, (q * 64 + lane) * V, end);
+  };
+  load(blockIdx.y);
+  for (long long row = blockIdx.y; row < J.rows; row += gridDim.y) {
     v4u in[N];
 #pragma unroll
-    for (int q = 0; q < N; ++q) in[q] = load16<TYPE>(x, first + q * 64 * V + lane * V, J.classes);
+    for (int q = 0; q < N; ++q) in[q] = next[q];
     const GradRow r = grad_row(J, row);
+    if (row + gridDim.y < J.rows) load(row + gridDim.y);
 #pragma unroll
-    for (int q = 0; q < N; ++q) {
-      const int c = first + q * 64 * V + lane * V;
-      union { v4u v; T e[V]; } out;
-#pragma unroll
-      for (int j = 0; j < V; ++j) out.e[j] = E::make(grad_of(r, E::get(in[q], j), c + j));
-      if (c + V <= J.classes) *(CNN_GLOBAL v4u_any*)(g + c) = out.v;
-      else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (c + j < J.classes) g[c + j] = out.e[j];
-      }
-    }
+    for (int q = 0; q < N; ++q) put_gradients<TYPE>(r, in[q], g + row * J.grad_stride, (q * 64 + lane) * V, end, first);
   }
 }
 
 constexpr long long GRID_MOST = 1 << 20;   // workgroups of a launch at most: rows beyond are looped over
 unsigned grid_of(long long work, long long per) { return (unsigned)std::min((work + per - 1) / per, GRID_MOST); }
 
-int lanes_of(int classes) {
-  int l = 4;
-  while (l < classes) l <<= 1;
+int lanes_of(int items) {   // the power of two
+  int l = 1;
+  while (l < items) l <<= 1;
   return l;
 }
 
@@ -661,31 +747,53 @@ hipError_t launch_scores_waves(hipStream_t stream, const ScoreJob& J) {
   return hipGetLastError();
 }
 
-#define CNN355_LANES(kernel)                                                                                                   \
-  switch (lanes_of(J.classes)) {                                                                                               \
-    case 4: hipLaunchKernelGGL((kernel<TYPE, 4>), dim3(grid_of(J.rows, ST / 4)), dim3(ST), 0, stream, J); break;               \
-    case 8: hipLaunchKernelGGL((kernel<TYPE, 8>), dim3(grid_of(J.rows, ST / 8)), dim3(ST), 0, stream, J); break;               \
-    case 16: hipLaunchKernelGGL((kernel<TYPE, 16>), dim3(grid_of(J.rows, ST / 16)), dim3(ST), 0, stream, J); break;            \
-    case 32: hipLaunchKernelGGL((kernel<TYPE, 32>), dim3(grid_of(J.rows, ST / 32)), dim3(ST), 0, stream, J); break;            \
-    default: hipLaunchKernelGGL((kernel<TYPE, 64>), dim3(grid_of(J.rows, ST / 64)), dim3(ST), 0, stream, J); break;            \
+#define CNN355_LANES(kernel, lanes)                                                                                   \
+  switch (lanes) {                                                                                                    \
+    case 1: hipLaunchKernelGGL((kernel<TYPE, 1>), dim3(grid_of(J.rows, ST)), dim3(ST), 0, stream, J); break;          \
+    case 2: hipLaunchKernelGGL((kernel<TYPE, 2>), dim3(grid_of(J.rows, ST / 2)), dim3(ST), 0, stream, J); break;      \
+    case 4: hipLaunchKernelGGL((kernel<TYPE, 4>), dim3(grid_of(J.rows, ST / 4)), dim3(ST), 0, stream, J); break;      \
+    case 8: hipLaunchKernelGGL((kernel<TYPE, 8>), dim3(grid_of(J.rows, ST / 8)), dim3(ST), 0, stream, J); break;      \
+    case 16: hipLaunchKernelGGL((kernel<TYPE, 16>), dim3(grid_of(J.rows, ST / 16)), dim3(ST), 0, stream, J); break;   \
+    case 32: hipLaunchKernelGGL((kernel<TYPE, 32>), dim3(grid_of(J.rows, ST / 32)), dim3(ST), 0, stream, J); break;   \
+    default: hipLaunchKernelGGL((kernel<TYPE, 64>), dim3(grid_of(J.rows, ST / 64)), dim3(ST), 0, stream, J); break;   \
   }
+
+// Whether the best of rows of up to 1024 classes come one by one (k_scores_rows) or sorted.  One by one they cost a row n_top
+// rounds of the lanes that share it, and few rows the rounds' latency.  us one by one / sorted: 100000 rows of 1000 bf16 5 best
+// 140 / 175, 16 best 327 / 199; of 100 5 best 22 / 172, fp32 64 best 138 / 247; of 64 16 best 27 / 48, fp32 64 best 89 / 49; of 16 all
+// 21 / 11; 300 rows of 300 bf16 16 best 11.6 / 9.1, 5 best the same.
+bool one_by_one(const ScoreJob& J) {
+  if (J.classes > SCORE_TILE) return false;
+  const int round = J.n_top * lanes_of((J.classes + 15) / 16);
+  return round <= 512 && (J.n_top <= 8 || (J.rows >= 4096 && 2 * J.classes > 3 * J.n_top));
+}
 
 template <int TYPE>
 hipError_t launch_scores_type(hipStream_t stream, const ScoreJob& J) {
-  if (J.classes > 64) {
+  if (one_by_one(J)) {
+    CNN355_LANES(k_scores_rows, lanes_of((J.classes + 15) / 16))
+  } else if (J.classes > 64) {
     return one_wavefront(J) ? launch_scores_waves<TYPE, 1>(stream, J) : launch_scores_waves<TYPE, 4>(stream, J);
+  } else {
+    switch (lanes_of(J.classes)) {   // (more than 8 best)
+      case 16: hipLaunchKernelGGL((k_scores_few<TYPE, 16>), dim3(grid_of(J.rows, ST / 16)), dim3(ST), 0, stream, J); break;
+      case 32: hipLaunchKernelGGL((k_scores_few<TYPE, 32>), dim3(grid_of(J.rows, ST / 32)), dim3(ST), 0, stream, J); break;
+      default: hipLaunchKernelGGL((k_scores_few<TYPE, 64>), dim3(grid_of(J.rows, ST / 64)), dim3(ST), 0, stream, J); break;
+    }
   }
-  CNN355_LANES(k_scores_few)
   return hipGetLastError();
 }
 
 template <int TYPE>
 hipError_t launch_scores_grad_type(hipStream_t stream, const ScoreGradJob& J) {
-  if (J.classes > 64) {
-    const long long tiles = (J.classes + SCORE_TILE - 1) / SCORE_TILE;
-    hipLaunchKernelGGL(k_scores_grad<TYPE>, dim3(grid_of(J.rows * tiles, ST / 64)), dim3(ST), 0, stream, J);
+  if (J.classes <= SCORE_TILE) {
+    CNN355_LANES(k_scores_grad_rows, lanes_of((J.classes + 15) / 16))
   } else {
-    CNN355_LANES(k_scores_grad_few)
+    // Workgroups that hold a row's tiles, and rows that are under way.  us with 2048 / 8192 workgroups / one for every four tiles:
+    // 2000 rows of 50001 fp16 102 / 84 / 90, 2048 of 131072 bf16 240 / 194 / 197, fp32 412 / 391 / 375, 20000 of 5000 bf16 129 / 104 / 116
+    const long long wide = (J.classes + 4 * SCORE_TILE - 1) / (4 * SCORE_TILE), rows = TYPE == ELEMENT_F32 ? J.rows : std::max(1ll, 8192 / wide);
+    const dim3 grid((unsigned)wide, (unsigned)std::min<long long>({J.rows, rows, 65535}));
+    hipLaunchKernelGGL(k_scores_grad<TYPE>, grid, dim3(ST), 0, stream, J);
   }
   return hipGetLastError();
 }
