@@ -67,6 +67,8 @@ hipError_t launch_scores(hipStream_t stream, const ScoreJob& J);
 hipError_t launch_scores_grad(hipStream_t stream, const ScoreGradJob& J);
 hipError_t launch_table(hipStream_t stream, const TensorJob& J, TensorEntry* at);
 hipError_t launch_squares(hipStream_t stream, const TensorJob& J, double* sums);
+bool list_is_small(const TensorJob& J, int op);
+hipError_t launch_small(hipStream_t stream, const TensorJob& J, int op, double max_norm, double lr, float* norm);
 hipError_t launch_norm(hipStream_t stream, const double* sums, int n, float* norm);
 hipError_t launch_scale(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, float* norm, int in_place);
 hipError_t launch_update(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, double lr, float* norm);
@@ -2004,7 +2006,7 @@ int over_gradients(const char* call, hipStream_t stream, const cnn_tensor* grads
   TensorJob J;
   J.table = nullptr; J.tensors = 0; J.chunks = 0; J.sums = 0; J.label = nullptr; J.classes = 0;
   hipError_t e = hipSuccess;
-  bool in_place = true;
+  bool in_place = true, apart = true;   // all of it, none of it
   size_t written = 0;
   auto flush = [&]() {
     if (live <= LIST_MOST || !J.tensors || e != hipSuccess) return;
@@ -2019,15 +2021,24 @@ int over_gradients(const char* call, hipStream_t stream, const cnn_tensor* grads
     t.from = (const CNN_GLOBAL void*)grads[i].d_data; t.to = (CNN_GLOBAL void*)(out ? out[i].d_data : nullptr);
     t.n = grads[i].n; t.type = grads[i].type; t.chunk = J.chunks;
     J.chunks += (unsigned)((grads[i].n * element_bytes(grads[i].type) + LIST_CHUNK - 1) / LIST_CHUNK);
-    in_place = in_place && t.from == (const CNN_GLOBAL void*)t.to;
+    const bool same = t.from == (const CNN_GLOBAL void*)t.to;
+    in_place = in_place && same;
+    apart = apart && !same;
   }
   flush();
   if (live > LIST_MOST) { J.table = (const CNN_GLOBAL TensorEntry*)table; J.tensors = (int)live; }
   J.sums = (int)std::max(1u, std::min(J.chunks, (unsigned)LIST_SUMS));
-  if (e == hipSuccess) e = launch_squares(stream, J, sums);
-  if (e == hipSuccess && apply == 0) e = launch_norm(stream, sums, J.sums, d_norm);
-  if (e == hipSuccess && apply == 1) e = launch_scale(stream, J, sums, max_norm, d_norm, in_place);
-  if (e == hipSuccess && apply == 2) e = launch_update(stream, J, sums, max_norm, lr, d_norm);
+  if (e == hipSuccess) {
+    if (apart && list_is_small(J, apply)) {
+      e = launch_small(stream, J, apply, max_norm, lr, d_norm);
+    } else {
+      e = launch_squares(stream, J, sums);
+      if (e == hipSuccess) {
+        e = apply == 0 ? launch_norm(stream, sums, J.sums, d_norm)
+          : apply == 1 ? launch_scale(stream, J, sums, max_norm, d_norm, in_place) : launch_update(stream, J, sums, max_norm, lr, d_norm);
+      }
+    }
+  }
   if (e != hipSuccess) return fail(nullptr, CNN_E_HIP, std::string(call) + ": " + hipGetErrorString(e));
   return CNN_OK;
 }
@@ -3127,8 +3138,13 @@ int cnn_train_many_clipped(cnn_t* net, const float* d_images, const int32_t* d_l
     int rc = run(net, a);
     if (rc) return rc;
     J.label = d_labels + t;
-    HIP_TRY(net, launch_squares(net->stream, J, net->d_clip_sums));
-    HIP_TRY(net, launch_update(net->stream, J, net->d_clip_sums, max_norm, lr, d_norms ? d_norms + t : nullptr));
+    float* norm = d_norms ? d_norms + t : nullptr;
+    if (list_is_small(J, 2)) {
+      HIP_TRY(net, launch_small(net->stream, J, 2, max_norm, lr, norm));
+    } else {
+      HIP_TRY(net, launch_squares(net->stream, J, net->d_clip_sums));
+      HIP_TRY(net, launch_update(net->stream, J, net->d_clip_sums, max_norm, lr, norm));
+    }
   }
   return CNN_OK;
 }

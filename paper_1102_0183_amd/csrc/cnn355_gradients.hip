@@ -28,6 +28,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // the sum of a double of every thread, in every thread
+template <int THREADS>
 __device__ __forceinline__ double sum_of_workgroup(double s, double* lds) {
   for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
   const int wave = threadIdx.x >> 6;
@@ -35,7 +36,7 @@ __device__ __forceinline__ double sum_of_workgroup(double s, double* lds) {
   __syncthreads();
   s = 0.0;
 #pragma unroll
-  for (int w = 0; w < GT / 64; ++w) s += lds[w];
+  for (int w = 0; w < THREADS / 64; ++w) s += lds[w];
   return s;
 }
 
@@ -50,8 +51,8 @@ struct Piece {   // a chunk of a tensor
 };
 
 // Chunk c's piece.  t: the tensor of a chunk that was looked up before (DOWN: of one behind c, else of one in front), then this one's.
-template <bool FAR, bool DOWN>
-__device__ __forceinline__ Piece piece_of(const TensorJob& J, unsigned i, int& t) {
+template <bool FAR, bool DOWN, class JOB>
+__device__ __forceinline__ Piece piece_of(const JOB& J, unsigned i, int& t) {
   Piece p = {nullptr, nullptr, 0, 0, 0};
   if (i >= J.chunks) return p;
   const unsigned c = DOWN ? J.chunks - 1 - i : i;
@@ -79,33 +80,40 @@ __device__ __forceinline__ Piece piece_of(const TensorJob& J, unsigned i, int& t
 }
 __device__ __forceinline__ bool whole(const Piece& p) { return p.n << (p.type == ELEMENT_F32 ? 2 : 1) == LIST_CHUNK; }
 
-// A workgroup's chunks, every gridDim.x-th of all, so that what is read side by side lies side by side (DOWN: from the last one
-// on): full(piece, its elements, 16 bytes a lane and load) or part(piece).  The next one is looked up while the loads of a chunk
-// are under way.  FOURS: types of 16 bits in loads of 8 bytes, two in the place of one of 16, so that the fp32 values that belong
-// to a wavefront's load lie side by side too.
-template <bool FAR, bool DOWN, bool FOURS, class Full, class Part>
-__device__ __forceinline__ void for_chunks(const TensorJob& J, Full full, Part part) {
+// GT threads and which of all chunks are theirs: every step-th, so that what is read side by side lies side by side.
+struct Share {
+  unsigned first, step;
+  int thread;
+};
+__device__ __forceinline__ Share share_of_workgroup() { return Share{blockIdx.x, gridDim.x, (int)threadIdx.x}; }
+
+// The chunks of a share (DOWN: from the last one on): full(piece, its elements, 16 bytes a lane and load) or part(piece).  The next
+// one is looked up while the loads of a chunk are under way (its loads too: no faster, and clipping of 320 tensors 288 us -> 304).
+// FOURS: types of 16 bits in loads of 8 bytes, two in the place of one of 16, so that the fp32 values that belong to a wavefront's
+// load lie side by side too.
+template <bool FAR, bool DOWN, bool FOURS, class JOB, class Full, class Part>
+__device__ __forceinline__ void for_chunks(const JOB& J, Share at, Full full, Part part) {
   int t = DOWN ? J.tensors - 1 : 0;
-  Piece p = piece_of<FAR, DOWN>(J, blockIdx.x, t);
-  for (unsigned i = blockIdx.x; i < J.chunks; i += gridDim.x) {
+  Piece p = piece_of<FAR, DOWN>(J, at.first, t);
+  for (unsigned i = at.first; i < J.chunks; i += at.step) {
     Piece next;
     if (whole(p)) {
       v4u r[NV];
       if (FOURS && p.type != ELEMENT_F32) {
 #pragma unroll
         for (int q = 0; q < 2 * NV; ++q) {
-          const v2u v = *(const CNN_GLOBAL v2u_any*)(p.from + (q * GT + threadIdx.x) * 8);
+          const v2u v = *(const CNN_GLOBAL v2u_any*)(p.from + (q * GT + at.thread) * 8);
           r[q >> 1][(q & 1) * 2] = v[0];
           r[q >> 1][(q & 1) * 2 + 1] = v[1];
         }
       } else {
 #pragma unroll
-        for (int q = 0; q < NV; ++q) r[q] = *(const CNN_GLOBAL v4u_any*)(p.from + (q * GT + threadIdx.x) * 16);
+        for (int q = 0; q < NV; ++q) r[q] = *(const CNN_GLOBAL v4u_any*)(p.from + (q * GT + at.thread) * 16);
       }
-      next = piece_of<FAR, DOWN>(J, i + gridDim.x, t);
+      next = piece_of<FAR, DOWN>(J, i + at.step, t);
       full(p, r);
     } else {
-      next = piece_of<FAR, DOWN>(J, i + gridDim.x, t);
+      next = piece_of<FAR, DOWN>(J, i + at.step, t);
       part(p);
     }
     p = next;
@@ -123,12 +131,11 @@ __device__ __forceinline__ void by_type(int type, F f) {
 }
 
 // ---- the sum of squares ----
-template <bool FAR>
-__global__ void __launch_bounds__(GT) k_squares(TensorJob J, CNN_GLOBAL double* sums) {
-  __shared__ double lds[GT / 64];
+template <bool FAR, class JOB>
+__device__ __forceinline__ double squares_of(const JOB& J, Share at) {
   double s = 0.0;
   for_chunks<FAR, false, false>(
-      J,
+      J, at,
       [&](const Piece& p, const v4u (&r)[NV]) {
         by_type(p.type, [&](auto type) {
           typedef Element<decltype(type)::value> E;
@@ -142,8 +149,8 @@ __global__ void __launch_bounds__(GT) k_squares(TensorJob J, CNN_GLOBAL double* 
         by_type(p.type, [&](auto type) {
           typedef Element<decltype(type)::value> E;
           const CNN_GLOBAL typename E::T* g = (const CNN_GLOBAL typename E::T*)p.from;
-          const int n = p.n / E::V, last = n * E::V + (int)threadIdx.x;
-          for (int i = threadIdx.x; i < n; i += GT) {
+          const int n = p.n / E::V, last = n * E::V + at.thread;
+          for (int i = at.thread; i < n; i += GT) {
             const v4u r = *(const CNN_GLOBAL v4u_any*)(g + i * E::V);
 #pragma unroll
             for (int j = 0; j < E::V; ++j) { const double v = E::get(r, j); s = fma(v, v, s); }
@@ -151,7 +158,13 @@ __global__ void __launch_bounds__(GT) k_squares(TensorJob J, CNN_GLOBAL double* 
           if (last < p.n) { const double v = E::get(g[last]); s = fma(v, v, s); }
         });
       });
-  s = sum_of_workgroup(s, lds);
+  return s;
+}
+
+template <class JOB, bool FAR>
+__global__ void __launch_bounds__(GT) k_squares(JOB J, CNN_GLOBAL double* sums) {
+  __shared__ double lds[GT / 64];
+  const double s = sum_of_workgroup<GT>(squares_of<FAR>(J, share_of_workgroup()), lds);
   if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 
@@ -166,7 +179,7 @@ __global__ void __launch_bounds__(128) k_table(TensorJob J, CNN_GLOBAL TensorEnt
 __device__ __forceinline__ double norm_of(const CNN_GLOBAL double* sums, int n, double* lds) {
   double s = 0.0;
   for (int i = threadIdx.x; i < n; i += GT) s += sums[i];
-  return sqrt(sum_of_workgroup(s, lds));
+  return sqrt(sum_of_workgroup<GT>(s, lds));
 }
 
 __global__ void __launch_bounds__(GT) k_norm(const CNN_GLOBAL double* sums, int n, CNN_GLOBAL float* norm) {
@@ -207,25 +220,22 @@ __device__ __forceinline__ v4u times(v4u r, const Factor& f) {
   return v;
 }
 
-// to = f g; to may be the gradients themselves
-template <bool FAR>
-__global__ void __launch_bounds__(GT) k_scale(TensorJob J, const CNN_GLOBAL double* sums, double max_norm, CNN_GLOBAL float* norm, int in_place) {
-  __shared__ double lds[GT / 64];
-  const double v = norm_of(sums, J.sums, lds);
-  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+// to = f g of a share's chunks, f = max_norm / v where that is less than 1; to may be the gradients themselves (in_place: all are)
+template <bool FAR, class JOB>
+__device__ __forceinline__ void scale(const JOB& J, Share at, double v, double max_norm, int in_place) {
   const bool clips = v < __builtin_inf() && v > max_norm;
   if (!clips && in_place) return;
   const Factor f = factor_of(clips ? max_norm / v : 1.0);
   // the last chunks first: they are the ones that the launch before read last, and may still be in a cache
   for_chunks<FAR, true, false>(
-      J,
+      J, at,
       [&](const Piece& p, const v4u (&r)[NV]) {
         by_type(p.type, [&](auto type) {
           constexpr int TYPE = decltype(type)::value;
           CNN_GLOBAL typename Element<TYPE>::T* o = (CNN_GLOBAL typename Element<TYPE>::T*)p.to + p.begin;
 #pragma unroll
           for (int q = 0; q < NV; ++q)
-            __builtin_nontemporal_store(clips ? times<TYPE>(r[q], f) : r[q], (CNN_GLOBAL v4u_any*)(o + (q * GT + threadIdx.x) * Element<TYPE>::V));
+            __builtin_nontemporal_store(clips ? times<TYPE>(r[q], f) : r[q], (CNN_GLOBAL v4u_any*)(o + (q * GT + at.thread) * Element<TYPE>::V));
         });
       },
       [&](const Piece& p) {
@@ -234,8 +244,8 @@ __global__ void __launch_bounds__(GT) k_scale(TensorJob J, const CNN_GLOBAL doub
           typedef typename Element<TYPE>::T T;
           const CNN_GLOBAL T* g = (const CNN_GLOBAL T*)p.from;
           CNN_GLOBAL T* o = (CNN_GLOBAL T*)p.to + p.begin;
-          const int n = p.n / V, last = n * V + (int)threadIdx.x;
-          for (int i = threadIdx.x; i < n; i += GT) {
+          const int n = p.n / V, last = n * V + at.thread;
+          for (int i = at.thread; i < n; i += GT) {
             const v4u r = *(const CNN_GLOBAL v4u_any*)(g + i * V);
             *(CNN_GLOBAL v4u_any*)(o + i * V) = clips ? times<TYPE>(r, f) : r;
           }
@@ -244,21 +254,14 @@ __global__ void __launch_bounds__(GT) k_scale(TensorJob J, const CNN_GLOBAL doub
       });
 }
 
-// to (weights) -= f lr g
-template <bool FAR>
-__global__ void __launch_bounds__(GT) k_update(TensorJob J, const CNN_GLOBAL double* sums, double max_norm, double lr, CNN_GLOBAL float* norm) {
-  __shared__ double lds[GT / 64];
-  if (J.label && (J.label[0] < 0 || J.label[0] >= J.classes)) {
-    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = 0.0f;
-    return;
-  }
-  const double v = norm_of(sums, J.sums, lds);
-  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+// to (weights) -= lr f g
+template <bool FAR, class JOB>
+__device__ __forceinline__ void update(const JOB& J, Share at, double v, double max_norm, double lr) {
   if (!(v < __builtin_inf())) return;
   const double f = -lr * (v > max_norm ? max_norm / v : 1.0);
   auto one = [&](float w, float g) { return (float)fma(f, (double)g, (double)w); };
   for_chunks<FAR, true, true>(
-      J,
+      J, at,
       [&](const Piece& p, const v4u (&r)[NV]) {
         by_type(p.type, [&](auto type) {
           typedef Element<decltype(type)::value> E;
@@ -266,22 +269,22 @@ __global__ void __launch_bounds__(GT) k_update(TensorJob J, const CNN_GLOBAL dou
           if constexpr (E::V == 4) {
             v4f o[NV];
 #pragma unroll
-            for (int q = 0; q < NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + threadIdx.x) * 4));
+            for (int q = 0; q < NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
 #pragma unroll
             for (int q = 0; q < NV; ++q) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) o[q][j] = one(o[q][j], E::get(r[q], j));
-              __builtin_nontemporal_store(o[q], (CNN_GLOBAL v4f_any*)(w + (q * GT + threadIdx.x) * 4));
+              __builtin_nontemporal_store(o[q], (CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
             }
           } else {
             v4f o[2 * NV];
 #pragma unroll
-            for (int q = 0; q < 2 * NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + threadIdx.x) * 4));
+            for (int q = 0; q < 2 * NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
 #pragma unroll
             for (int q = 0; q < 2 * NV; ++q) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) o[q][j] = one(o[q][j], E::get(r[q >> 1], (q & 1) * 4 + j));
-              __builtin_nontemporal_store(o[q], (CNN_GLOBAL v4f_any*)(w + (q * GT + threadIdx.x) * 4));
+              __builtin_nontemporal_store(o[q], (CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
             }
           }
         });
@@ -291,12 +294,71 @@ __global__ void __launch_bounds__(GT) k_update(TensorJob J, const CNN_GLOBAL dou
           typedef Element<decltype(type)::value> E;
           const CNN_GLOBAL typename E::T* g = (const CNN_GLOBAL typename E::T*)p.from;
           CNN_GLOBAL float* w = (CNN_GLOBAL float*)p.to + p.begin;
-          for (int i = threadIdx.x; i < p.n; i += GT) w[i] = one(w[i], E::get(g[i]));
+          for (int i = at.thread; i < p.n; i += GT) w[i] = one(w[i], E::get(g[i]));
         });
       });
 }
 
+// Whether the gradients are of an image that is passed over for its label (its norm is 0)
+__device__ __forceinline__ bool passed_over(const TensorHead& J, CNN_GLOBAL float* norm) {
+  if (!J.label || (J.label[0] >= 0 && J.label[0] < J.classes)) return false;
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = 0.0f;
+  return true;
+}
+
+template <class JOB, bool FAR>
+__global__ void __launch_bounds__(GT) k_scale(JOB J, const CNN_GLOBAL double* sums, double max_norm, CNN_GLOBAL float* norm, int in_place) {
+  __shared__ double lds[GT / 64];
+  const double v = norm_of(sums, J.sums, lds);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+  scale<FAR>(J, share_of_workgroup(), v, max_norm, in_place);
+}
+
+template <class JOB, bool FAR>
+__global__ void __launch_bounds__(GT) k_update(JOB J, const CNN_GLOBAL double* sums, double max_norm, double lr, CNN_GLOBAL float* norm) {
+  __shared__ double lds[GT / 64];
+  if (passed_over(J, norm)) return;
+  const double v = norm_of(sums, J.sums, lds);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+  update<FAR>(J, share_of_workgroup(), v, max_norm, lr);
+}
+
+// Small lists in one launch: every workgroup, four groups of GT threads, adds the squares of all chunks for itself (the same way, so
+// that they agree) and goes over its own.  OP 0: the norm alone, 1: scale (not in place: another workgroup may still read what
+// one has written), 2: update.
+constexpr int SMALL_GROUPS = 4;
+template <class JOB, int OP>
+__global__ void __launch_bounds__(GT * SMALL_GROUPS) k_small(JOB J, double max_norm, double lr, CNN_GLOBAL float* norm) {
+  __shared__ double lds[SMALL_GROUPS * GT / 64];
+  if (passed_over(J, norm)) return;
+  const unsigned group = __builtin_amdgcn_readfirstlane(threadIdx.x / GT);
+  const int thread = threadIdx.x % GT;
+  const double v = sqrt(sum_of_workgroup<GT * SMALL_GROUPS>(squares_of<false>(J, Share{group, SMALL_GROUPS, thread}), lds));
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+  const Share own = {blockIdx.x * SMALL_GROUPS + group, gridDim.x * SMALL_GROUPS, thread};
+  if (OP == 1) scale<false>(J, own, v, max_norm, 0);
+  if (OP == 2) update<false>(J, own, v, max_norm, lr);
+}
+
 constexpr unsigned APPLY_GRID = 2048;
+
+// f(the argument that a kernel takes, whether its entries lie in memory)
+template <class F>
+hipError_t with_job(const TensorJob& J, F f) {
+  if (!J.table && J.tensors > LIST_FEW) {
+    f(J, std::false_type());
+  } else {
+    TensorJobFew few;
+    static_cast<TensorHead&>(few) = J;
+    if (J.table) {
+      f(few, std::true_type());
+    } else {
+      for (int t = 0; t < J.tensors; ++t) few.e[t] = J.e[t];
+      f(few, std::false_type());
+    }
+  }
+  return hipGetLastError();
+}
 
 unsigned apply_grid(const TensorJob& J) { return std::max(1u, std::min(J.chunks, APPLY_GRID)); }
 
@@ -308,9 +370,22 @@ hipError_t launch_table(hipStream_t stream, const TensorJob& J, TensorEntry* at)
 }
 
 hipError_t launch_squares(hipStream_t stream, const TensorJob& J, double* sums) {
-  if (J.table) hipLaunchKernelGGL(k_squares<true>, dim3((unsigned)J.sums), dim3(GT), 0, stream, J, (CNN_GLOBAL double*)sums);
-  else hipLaunchKernelGGL(k_squares<false>, dim3((unsigned)J.sums), dim3(GT), 0, stream, J, (CNN_GLOBAL double*)sums);
-  return hipGetLastError();
+  return with_job(J, [&](const auto& job, auto far) {
+    hipLaunchKernelGGL((k_squares<std::decay_t<decltype(job)>, decltype(far)::value>), dim3((unsigned)J.sums), dim3(GT), 0, stream, job, (CNN_GLOBAL double*)sums);
+  });
+}
+
+bool list_is_small(const TensorJob& J, int op) { return !J.table && J.chunks <= (op == 0 ? 32u : op == 1 ? 26u : 20u); }
+
+hipError_t launch_small(hipStream_t stream, const TensorJob& J, int op, double max_norm, double lr, float* norm) {
+  const dim3 grid(op == 0 ? 1 : std::max(1u, (J.chunks + SMALL_GROUPS - 1) / SMALL_GROUPS)), threads(GT * SMALL_GROUPS);
+  CNN_GLOBAL float* n = (CNN_GLOBAL float*)norm;
+  return with_job(J, [&](const auto& job, auto) {
+    typedef std::decay_t<decltype(job)> JOB;
+    if (op == 0) hipLaunchKernelGGL((k_small<JOB, 0>), grid, threads, 0, stream, job, max_norm, lr, n);
+    else if (op == 1) hipLaunchKernelGGL((k_small<JOB, 1>), grid, threads, 0, stream, job, max_norm, lr, n);
+    else hipLaunchKernelGGL((k_small<JOB, 2>), grid, threads, 0, stream, job, max_norm, lr, n);
+  });
 }
 
 hipError_t launch_norm(hipStream_t stream, const double* sums, int n, float* norm) {
@@ -319,17 +394,17 @@ hipError_t launch_norm(hipStream_t stream, const double* sums, int n, float* nor
 }
 
 hipError_t launch_scale(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, float* norm, int in_place) {
-  const CNN_GLOBAL double* s = (const CNN_GLOBAL double*)sums;
-  if (J.table) hipLaunchKernelGGL(k_scale<true>, dim3(apply_grid(J)), dim3(GT), 0, stream, J, s, max_norm, (CNN_GLOBAL float*)norm, in_place);
-  else hipLaunchKernelGGL(k_scale<false>, dim3(apply_grid(J)), dim3(GT), 0, stream, J, s, max_norm, (CNN_GLOBAL float*)norm, in_place);
-  return hipGetLastError();
+  return with_job(J, [&](const auto& job, auto far) {
+    hipLaunchKernelGGL((k_scale<std::decay_t<decltype(job)>, decltype(far)::value>), dim3(apply_grid(J)), dim3(GT), 0, stream, job,
+                       (const CNN_GLOBAL double*)sums, max_norm, (CNN_GLOBAL float*)norm, in_place);
+  });
 }
 
 hipError_t launch_update(hipStream_t stream, const TensorJob& J, const double* sums, double max_norm, double lr, float* norm) {
-  const CNN_GLOBAL double* s = (const CNN_GLOBAL double*)sums;
-  if (J.table) hipLaunchKernelGGL(k_update<true>, dim3(apply_grid(J)), dim3(GT), 0, stream, J, s, max_norm, lr, (CNN_GLOBAL float*)norm);
-  else hipLaunchKernelGGL(k_update<false>, dim3(apply_grid(J)), dim3(GT), 0, stream, J, s, max_norm, lr, (CNN_GLOBAL float*)norm);
-  return hipGetLastError();
+  return with_job(J, [&](const auto& job, auto far) {
+    hipLaunchKernelGGL((k_update<std::decay_t<decltype(job)>, decltype(far)::value>), dim3(apply_grid(J)), dim3(GT), 0, stream, job,
+                       (const CNN_GLOBAL double*)sums, max_norm, lr, (CNN_GLOBAL float*)norm);
+  });
 }
 
 }  // namespace cnn355

@@ -49,6 +49,7 @@ struct ScoreGradJob {
 
 // ---- many tensors -------------------------------------------------------------------------------
 constexpr int LIST_MOST = 120;     // tensors of a kernel's argument (below 4 KB)
+constexpr int LIST_FEW = 16;       // tensors of a smaller one
 constexpr int LIST_CHUNK = 16384;  // bytes: gradients are cut into chunks of so many
 constexpr int LIST_SUMS = 1024;    // workgroups that leave a sum, at most
 
@@ -59,14 +60,19 @@ struct TensorEntry {
   unsigned int chunk;              // its first chunk among those of all tensors
   int type;
 };
-struct TensorJob {
+struct TensorHead {
   const CNN_GLOBAL TensorEntry* table;   // where they do not fit in `e`
   int tensors;
   unsigned int chunks;             // of all tensors
   int sums;                        // workgroups that leave a sum
   const CNN_GLOBAL int* label;     // null, or of the image that the gradients are of: outside [0, classes) it is passed over
   int classes;
-  TensorEntry e[LIST_MOST];
 };
+template <int N>
+struct TensorsOf : TensorHead {
+  TensorEntry e[N];
+};
+typedef TensorsOf<LIST_MOST> TensorJob;
+typedef TensorsOf<LIST_FEW> TensorJobFew;   // (a launch of a small argument takes the host less)
 
 }  // namespace cnn355
