@@ -325,16 +325,29 @@ __device__ __forceinline__ void pick(Best& b, Picking& L, const RowAt<TYPE>& row
         const int at = (first + (at_lane >> 6) * step) * SCORE_TILE + (k / V) * 64 * V + (at_lane & 63) * V + k % V;
         key[u] = w < waiting && at >= row.lead && at < row.end ? key_of_any(E::get(row.at[at]), at - row.lead) : 0;
       }
-#pragma unroll 1
-      for (int u = 0; u < 8; ++u) {
-        const u64 k = key[0], take = __ballot(k > b.bar);
+      // all of them where they are few, as they mostly are; else four lanes' at a time
+      int n = b.held;
 #pragma unroll
-        for (int j = 0; j < 7; ++j) key[j] = key[j + 1];
-        if (k > b.bar) L.held[b.held + place_in(take)] = k;
-        b.held += __popcll(take);
-        const bool end = w0 + (u + 1) * 4 >= waiting;
-        while (b.held >= 64 || (end && finish && b.held)) take_held(b, L, n_top);
-        if (end) break;
+      for (int u = 0; u < 8; ++u) n += __popcll(__ballot(key[u] > b.bar));
+      const bool few = n <= HELD;
+      if (few) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const u64 take = __ballot(key[u] > b.bar);
+          if (key[u] > b.bar) L.held[b.held + place_in(take)] = key[u];
+          b.held += __popcll(take);
+        }
+      }
+#pragma unroll 1
+      for (int u = few ? 7 : 0; u < 8; ++u) {
+        if (!few) {
+          const u64 k = key[0], take = __ballot(k > b.bar);
+#pragma unroll
+          for (int j = 0; j < 7; ++j) key[j] = key[j + 1];
+          if (k > b.bar) L.held[b.held + place_in(take)] = k;
+          b.held += __popcll(take);
+        }
+        while (b.held >= 64 || (u == 7 && finish && w0 + 32 >= waiting && b.held)) take_held(b, L, n_top);
       }
     }
     waiting = 0;
@@ -359,10 +372,12 @@ __device__ __forceinline__ void load_tile(v4u (&r)[16 / Element<TYPE>::V], const
 
 // Tiles first, first + step, ... of a row, below `last`: the wavefront's sums, lane by lane, and its best.
 //
-// In the usual tile the exponent is one operation, d = x / ln 2 - r with r = m / ln 2 as rounded: every e is too large by the
-// same 2^(m / ln 2 - r), which is taken out at the end.  A masked class gives 0 (-inf) there and values near the type's lowest
+// In the usual tile the exponent is one operation, d = x / ln 2 - r, with a lane's r as m / ln 2 was when it was last above r by
+// more than GROWTH (then both sums go to the new r): every e is too large by the same 2^(m / ln 2 - r), which is taken out at
+// the end.  A masked class gives 0 (-inf) there and values near the type's lowest
 // and highest leave the range of d; a tile that has any shows it in its sums, is done again with d = (x - m) / ln 2 and the
 // product of e and d clamped, and so are those behind it (two operations more for each class).
+constexpr float GROWTH = 8.0f;   // (t is off by r's distance from m times the rounding of s)
 template <int TYPE, bool ENTROPY, bool TOP>
 __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step, int last, int n_top, Sums& a, Best& b, Picking* L) {
 #pragma clang fp contract(off)   // (r is the rounded product in the difference of two of them, too)
@@ -380,14 +395,12 @@ __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step
       a.s *= f;
     }
   };
-  v4u next[N];
-  if (first < last) load_tile<TYPE>(next, row, first);
   int in_segment = 0;
-  for (int tile = first; tile < last; tile += step) {
+  auto one = [&](v4u (&next)[N], int tile) {   // and asks for the one after the next
     float x[16];
 #pragma unroll
     for (int k = 0; k < 16; ++k) x[k] = E::get(next[k / V], k % V);
-    if (tile + step < last) load_tile<TYPE>(next, row, tile + step);
+    if (tile + 2 * step < last) load_tile<TYPE>(next, row, tile + 2 * step);
     float top[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -399,15 +412,21 @@ __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step
     }
     const float m = max3(a.m, top[0], top[1]);
     if (!rough) {
-      const float to = m * LOG2E, d0 = r - to, f = __builtin_amdgcn_exp2f(d0);
-      float s = a.s * f, t = fmaf(fmaxf(d0, FAR), a.s, a.t) * f;
+      float to = r, s = a.s, t = a.t;
+      const bool grown = fmaf(m, LOG2E, -r) > GROWTH;
+      if (__ballot(grown)) {
+        to = grown ? m * LOG2E : r;
+        const float d0 = r - to, f = __builtin_amdgcn_exp2f(d0);
+        t = fmaf(fmaxf(d0, FAR), s, t) * f;
+        s *= f;
+      }
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
         const float d = fmaf(x[k], LOG2E, -to), e = __builtin_amdgcn_exp2f(d);
         s += e;
         if (ENTROPY) t = fmaf(e, d, t);
       }
-      const float sure = ENTROPY ? t : s;
+      const float sure = ENTROPY ? t + s : s;   // (both: else the sum of all e is put off behind the branch, and every e kept for it)
       if (__ballot(!(sure - sure == 0.0f)) == 0) {
         r = to;
         a = Sums{m, s, t};
@@ -428,10 +447,19 @@ __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step
     if (TOP) {
       const unsigned bits = __builtin_bit_cast(unsigned, max3(top[0], top[1], top[1]));
       L->largest[in_segment++][threadIdx.x & 63] = (unsigned short)((TYPE == ELEMENT_BF16 || (int)bits < 0 ? bits : bits + 0xffffu) >> 16);
-      if (in_segment == SEGMENT || tile + step >= last) {
-        pick<TYPE>(b, *L, row, largest[0], largest[1], tile - (in_segment - 1) * step, step, in_segment, tile + step >= last, n_top);
-        in_segment = 0;
-      }
+    }
+  };
+  v4u even[N], odd[N];
+  if (first < last) load_tile<TYPE>(even, row, first);
+  if (first + step < last) load_tile<TYPE>(odd, row, first + step);
+  for (int tile = first; tile < last; tile += 2 * step) {
+    one(even, tile);
+    if (tile + step < last) one(odd, tile + step);
+    const bool end = tile + 2 * step >= last;
+    if (TOP && (in_segment == SEGMENT || end)) {
+      const int begun = tile + (tile + step < last ? step : 0) - (in_segment - 1) * step;
+      pick<TYPE>(b, *L, row, largest[0], largest[1], begun, step, in_segment, end, n_top);
+      in_segment = 0;
     }
   }
   if (!rough) settle();
