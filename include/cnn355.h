@@ -452,12 +452,12 @@ int cnn_class_scores_grad(void* hip_stream, const void* d_logits, int type, size
 /* ---- gradients of many tensors: their norm, clipping, the clipped update ---------------------------
  * With N = sqrt(sum of the squares of all elements of all tensors) and f = max_norm / N where N > max_norm, else 1:
  *   cnn_gradient_norm:  *d_norm = N
- *   cnn_clip_gradients: out = f g, rounded once, of the gradients' types.  host_out == NULL: in place (not written
- *                       at all where f is 1)
+ *   cnn_clip_gradients: out = f g, of the gradients' types, rounded to fp32 and from there to them.  host_out == NULL:
+ *                       in place (not written at all where f is 1)
  *   cnn_clipped_update: w <- w - lr f g for fp32 weights and gradients of any type (Sec. 3.4's adjustment)
  * A norm that is infinite or NaN changes nothing: out = g, weights stay, and *d_norm (NULL where it is not wanted,
- * but in cnn_gradient_norm) tells.  Squares, sums and products with f are double; the result depends on the list
- * alone, bit for bit.
+ * but in cnn_gradient_norm) tells.  Squares, their sum, f and the update's product are double; the result depends on
+ * the list alone, bit for bit.
  * host_grads, host_out, host_weights: host arrays of n tensors (read before the call returns) of device memory,
  * elements contiguous, sizes and types (weights: CNN_TYPE_F32) of the same order; a size may be 0.  What is written
  * must overlap nothing else in the call, but out[i] may be grads[i].  d_scratch: device memory, 256-byte aligned, at

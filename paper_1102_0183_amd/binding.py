@@ -264,7 +264,8 @@ class Tensor(C.Structure):
 class TensorList:
     """A list of device tensors of one device for the calls below, made once and used for every step: float32, bfloat16 or float16,
     each dense (contiguous, or a permutation of it: the order of elements does not matter to a norm; lists that go together must
-    have the same one).  The tensors are kept."""
+    have the same one).  The tensors are kept, and have to keep their memory: one that is given other memory (resize_, .data = ..,
+    .grad = None and a new one) needs a new list."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)

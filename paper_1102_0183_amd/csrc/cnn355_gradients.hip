@@ -6,7 +6,7 @@
 // Two launches: every workgroup of the first leaves the sum of its chunks in memory, every workgroup of the second adds all
 // those sums (the same way, so that all agree on N to the last bit and a call gives the same bits again) and goes over its
 // chunks.  Squares and sums are doubles: no gradient that a float holds overflows or vanishes in its square, and the order of
-// a thousand million terms does not show.  So is the product with the factor, which is rounded once.
+// a thousand million terms does not show.  So is an update's product with the factor, rounded once with the difference.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -115,7 +115,7 @@ def test_rows_start_anywhere(rows, n, top, pad, offset, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n", [10, 64, 200, 3000, 20000])
+@pytest.mark.parametrize("n", [10, 64, 200, 3000, 20000, 90000])
 def test_masked_classes_empty_rows_lowest_values_infinities_and_nan(n, dtype):
     import torch
     x, labels = _rows(12, n, dtype, 3)
@@ -152,6 +152,61 @@ def test_ties_go_to_the_lower_index_and_order_does_not_matter(n, dtype):
     labels = torch.full((len(rows),), n - 1, dtype=torch.int32, device="cuda:0")
     for top in (1, 13, 50 if n == 50 else 64):
         _check(x, labels, top, _call(x, labels, top))
+
+
+def _sampled(x, labels, top, out, at):
+    """_check of a few rows."""
+    import torch
+    i = torch.tensor(sorted(set(at)), device="cuda:0")
+    _check(x[i], labels[i], top, {k: v[i] for k, v in out.items()})
+
+
+@pytest.mark.parametrize("rows,n,top,dtype", [
+    (4100, 100, 20, "bfloat16"), (5000, 40, 16, "float32"), (4097, 300, 12, "float16"), (4099, 128, 64, "float32"), (4096, 64, 64, "bfloat16"),
+    (4096, 8300, 3, "bfloat16"), (4097, 32768, 20, "float16"), (4097, 33000, 64, "bfloat16"), (5000, 5000, 1, "float32"), (9000, 16, 16, "float16"),
+])
+def test_many_rows(rows, n, top, dtype):
+    x, labels = _rows(rows, n, dtype, n, pad=n % 2)
+    x[rows // 3, 1:] = -math.inf
+    x[rows // 2, 3] = math.nan
+    _sampled(x, labels, top, _call(x, labels, top), [0, 1, rows // 3, rows // 2, rows - 2, rows - 1] + list(range(5, rows, rows // 9)))
+
+
+@pytest.mark.parametrize("rows,n,top,dtype", [
+    ((1 << 28) + 77, 2, 1, "float16"),          # more rows than a launch has places for, in every kernel
+    ((1 << 24) + 9, 10, 9, "bfloat16"),
+    ((1 << 22) + 5, 1030, 9, "bfloat16"),
+    ((1 << 20) + 3, 4100, 0, "bfloat16"),
+])
+def test_more_rows_than_a_launch_holds(rows, n, top, dtype):
+    """Rows go on behind the last workgroup; their places pass 32 bits.  (Rows repeat 65536 different ones.)"""
+    import torch
+    some, l = _rows(65536 + 1, n, dtype, 3)
+    x = torch.empty(rows, n, dtype=some.dtype, device="cuda:0")
+    for a in range(0, rows, some.shape[0]):
+        x[a:a + some.shape[0]] = some[:rows - a]
+    labels = l.repeat(-(-rows // some.shape[0]))[:rows].contiguous()
+    out = _call(x, labels, top)
+    at = [0, 1, rows - 1, rows - 2, rows // 2, (rows // 4) | 1, rows - 70000 if rows > 70000 else 3]
+    _sampled(x, labels, top, out, at)
+    first = _call(some[:1000].contiguous(), l[:1000].contiguous(), top)
+    k = (rows // some.shape[0] - 1) * some.shape[0]
+    there, here = out["lp"][k:k + 1000], first["lp"]      # (the sums in another order, it may be)
+    assert ((there - here).abs() <= 2 * (_terms(rows, n) + 100) * U * (2 + 2 * math.log(n) + here.abs())).all()
+
+
+@pytest.mark.parametrize("n,top", [(700, 5), (5000, 20)])
+def test_rows_that_lie_far_apart(n, top):
+    """Offsets beyond 32 bits, of elements and of bytes."""
+    import torch
+    stride = (1 << 31) + 3
+    wide = torch.empty(stride + n, dtype=torch.bfloat16, device="cuda:0")
+    x = wide.as_strided((2, n), (stride, 1))
+    x.copy_(_rows(2, n, "bfloat16", 6)[0])
+    labels = torch.tensor([n - 1, 3], dtype=torch.int32, device="cuda:0")
+    _check(x, labels, top, _call(x, labels, top))
+    g = torch.randn(2, 2, device="cuda:0")
+    _check_grad(x, labels, g[0].contiguous(), g[1].contiguous(), x)      # in place
 
 
 @pytest.mark.parametrize("dtype", TYPES)

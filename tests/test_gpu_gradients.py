@@ -163,6 +163,37 @@ def test_tensors_that_are_dense_in_another_order():
             binding.TensorList([bad])
 
 
+def test_a_tensor_beyond_32_bits():
+    """2^31 + 7 elements: the last ones count, are clipped and are used."""
+    import torch
+    n = (1 << 31) + 7
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda:0")
+    g[-3:] = 2.0
+    g[5] = 1.0
+    small = torch.full((3,), 2.0, device="cuda:0")
+    norm = math.sqrt(12 + 1 + 12)
+    assert abs(float(_run_norm([small, g])) - norm) <= norm * U
+    w = [torch.ones(3, device="cuda:0"), torch.ones(n, device="cuda:0")]
+    binding.clipped_update(binding.TensorList(w), binding.TensorList([small, g]), 1.0, 0.5 * norm, _scratch(2))
+    assert float(w[1][-1]) == 0.0 and float(w[1][5]) == 0.5 and float(w[1][-4]) == 1.0 and float(w[1].sum(dtype=torch.float64)) == n - 3 - 0.5
+    del w
+    binding.clip_gradients(binding.TensorList([small, g]), 0.5 * norm, _scratch(2))
+    assert (g[-3:] == 1.0).all() and float(g[5]) == 0.5 and (small == 1.0).all() and float(g[-4]) == 0.0
+
+
+@pytest.mark.parametrize("counts", [[300] * 3, [9000] * 40])
+def test_some_in_place_and_some_not(counts):
+    import torch
+    grads, _ = _tensors(counts, ["float32"] * len(counts), 2)
+    before = [g.clone() for g in grads]
+    norm = _norm(grads)
+    out = [g if k % 2 else torch.zeros_like(g) for k, g in enumerate(grads)]
+    for limit in (2 * norm, 0.1 * norm):
+        binding.clip_gradients(binding.TensorList(grads), limit, _scratch(len(counts)), out=binding.TensorList(out))
+        _check_clip(before, out, norm, limit)
+        assert all(torch.equal(g, b) for k, (g, b) in enumerate(zip(grads, before)) if k % 2 == 0)
+
+
 def test_streams_and_a_captured_step():
     import torch
     counts = [20, 320, 40, 20000, 150, 54000, 10, 1500] * 20          # two launches of tensors
