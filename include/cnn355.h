@@ -459,10 +459,11 @@ int cnn_class_scores_grad(void* hip_stream, const void* d_logits, int type, size
  * but in cnn_gradient_norm) tells.  Squares, their sum, f and the update's product are double; the result depends on
  * the list alone, bit for bit.
  * host_grads, host_out, host_weights: host arrays of n tensors (read before the call returns) of device memory,
- * elements contiguous, sizes and types (weights: CNN_TYPE_F32) of the same order; a size may be 0.  What is written
- * must overlap nothing else in the call, but out[i] may be grads[i].  d_scratch: device memory, 256-byte aligned, at
- * least cnn_gradient_scratch_bytes(n) (host-only), free once the stream has passed the call; calls that may
- * overlap need one each.  max_norm >= 0 (inf: never clipped), lr finite.  Asynchronous; nothing is allocated.
+ * elements contiguous, sizes and types (weights: CNN_TYPE_F32) of the same order; a size may be 0.  At most 2^24
+ * tensors, of 2^43 elements together.  What is written must overlap nothing else in the call, but out[i] may be
+ * grads[i].  d_scratch: device memory, 256-byte aligned, at least cnn_gradient_scratch_bytes(n) (host-only), free once
+ * the stream has passed the call; calls that may overlap need one each.  max_norm >= 0 (inf: never clipped), lr
+ * finite.  Asynchronous; nothing is allocated.
  * Errors: CNN_E_ARG, CNN_E_WORKSPACE, CNN_E_HIP; the message is cnn_last_error(NULL)'s. */
 typedef struct cnn_tensor {
   void* d_data;

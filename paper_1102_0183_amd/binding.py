@@ -307,7 +307,11 @@ def _over_gradients(grads, other, d_norm, d_scratch):
     """(device, address of the norm, scratch, its bytes) of a call, its lists looked over."""
     if _f32 is None:
         _know_torch()
-    dev = grads.device or (d_norm if d_norm is not None else d_scratch).device
+    dev = grads.device
+    if dev is None:
+        some = d_norm if d_norm is not None else d_scratch
+        assert some is not None, "expected scratch memory"
+        dev = some.device
     if other is not None:
         assert len(other) == len(grads) and other.device == grads.device and other.orders == grads.orders, \
             "lists that go together have the same tensors, laid out alike"
@@ -629,7 +633,7 @@ class Cnn:
         if _f32 is None:
             _know_torch()
         dev = d_images.device
-        assert d_images.is_cuda and d_images.dtype == torch.float32 and d_images.is_contiguous()
+        assert dev == self.workspace.device and d_images.dtype == torch.float32 and d_images.is_contiguous()
         assert d_images.numel() >= n * self.image_size
         scratch, nbytes = _scratch_of(d_scratch, dev)
         some = d_top if d_top is not None else d_top_log_probs

@@ -1949,6 +1949,10 @@ int batch_plan(cnn* net, size_t batch, std::shared_ptr<const BatchKept>& out) {
 
 // ---- many tensors ----------------------------------------------------------------------------------
 namespace {
+// (2^31 chunks, and one of every tensor's that is not full: their numbers, and the step beyond the last, stay below 2^32)
+constexpr size_t LIST_TENSORS = (size_t)1 << 24;
+constexpr unsigned long long LIST_ELEMENTS = 1ull << 43;
+
 // What is wrong with a list (NULL: nothing).  to: what is written, or null; weights: to is fp32 whatever the gradients are.
 const char* check_list(const cnn_tensor* from, const cnn_tensor* to, size_t n, bool weights) {
   if (n && !from) return "NULL list";
@@ -1956,7 +1960,7 @@ const char* check_list(const cnn_tensor* from, const cnn_tensor* to, size_t n, b
   for (size_t i = 0; i < n; ++i) {
     const cnn_tensor& g = from[i];
     if (g.type != CNN_TYPE_F32 && g.type != CNN_TYPE_BF16 && g.type != CNN_TYPE_F16) return "unknown type";
-    if (g.n > (size_t)1 << 44 || (all += g.n) > (1ull << 44)) return "too many elements";
+    if (g.n > LIST_ELEMENTS || (all += g.n) > LIST_ELEMENTS) return "too many elements";
     if (g.n && (!g.d_data || (uintptr_t)g.d_data % element_bytes(g.type))) return "a tensor is NULL or misaligned";
     if (!to) continue;
     if (to[i].n != g.n) return "sizes of the two lists differ";
@@ -1986,7 +1990,7 @@ const char* check_list(const cnn_tensor* from, const cnn_tensor* to, size_t n, b
 // apply 0: the norm only, 1: scale, 2: update
 int over_gradients(const char* call, hipStream_t stream, const cnn_tensor* grads, const cnn_tensor* out, size_t n, int apply,
                    float max_norm, float lr, float* d_norm, void* d_scratch, size_t scratch_bytes) {
-  if (n > (size_t)1 << 24) return fail(nullptr, CNN_E_ARG, std::string(call) + ": too many tensors");
+  if (n > LIST_TENSORS) return fail(nullptr, CNN_E_ARG, std::string(call) + ": too many tensors");
   const char* why = nullptr;
   try {
     why = check_list(grads, out, n, apply == 2);
@@ -2905,7 +2909,7 @@ int cnn_class_scores_grad(void* hip_stream, const void* d_logits, int type, size
 // ---- many tensors ----------------------------------------------------------------------------------
 int cnn_gradient_scratch_bytes(size_t n, size_t* bytes) {
   if (!bytes) return fail(nullptr, CNN_E_ARG, "cnn_gradient_scratch_bytes: NULL argument");
-  if (n > (size_t)1 << 24) return fail(nullptr, CNN_E_ARG, "cnn_gradient_scratch_bytes: too many tensors");
+  if (n > LIST_TENSORS) return fail(nullptr, CNN_E_ARG, "cnn_gradient_scratch_bytes: too many tensors");
   *bytes = LIST_SUMS * sizeof(double) + (n > LIST_MOST ? n * sizeof(TensorEntry) : 0);
   return CNN_OK;
 }

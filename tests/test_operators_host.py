@@ -137,3 +137,19 @@ def test_scratch_of_lists():
     with pytest.raises(binding.CnnError):
         binding.gradient_scratch_bytes(1 << 30)
     assert L.cnn_gradient_norm(None, g, 1 << 30, P, P, 1 << 40) == E_ARG
+
+
+def test_lists_of_more_chunks_than_are_counted():
+    """2^43 elements are 2^31 chunks; the kernels count them, and the step beyond the last, in 32 bits."""
+    L, n = binding.lib(), binding.gradient_scratch_bytes(2)
+    for counts in ([1 << 44], [(1 << 43) + 1], [1 << 43, 1], [1 << 42] * 4):
+        g = _list(*[(P, c, B) for c in counts])
+        assert L.cnn_gradient_norm(None, g, len(counts), P, P, n) == E_ARG, counts
+
+
+def test_an_empty_list_needs_a_device():
+    empty = binding.TensorList([])
+    for call in (lambda: binding.clip_gradients(empty, 1.0, None), lambda: binding.clipped_update(empty, empty, 0.1, 1.0, None),
+                 lambda: binding.gradient_norm(empty, None, None)):
+        with pytest.raises(AssertionError):
+            call()
