@@ -6,7 +6,8 @@
 //
 // One pass over the row: every lane keeps the largest value m it has seen, s = sum of exp(x - m) and t = sum of
 // exp(x - m) (x - m), and takes both to a new m by the factor exp(m - m'): s' = s f, t' = (t + (m - m') s) f.  Lanes,
-// wavefronts and workgroups that share a row join their three numbers in the same way.  All of it is held in 32 bits.
+// wavefronts and workgroups that share a row join their three numbers in the same way.  All of it is held in 32 bits.  (Long rows
+// take m in steps, so that most tiles need no factor: at `scan`.)
 //
 // The best classes ride along.  A wavefront keeps the best so far sorted over its lanes, as 64-bit keys (value, then the
 // lower index) whose order is that of whole numbers.  Every 32 tiles it picks out what reaches the n_top-th of its lanes'
@@ -374,9 +375,9 @@ __device__ __forceinline__ void load_tile(v4u (&r)[16 / Element<TYPE>::V], const
 //
 // In the usual tile the exponent is one operation, d = x / ln 2 - r, with a lane's r as m / ln 2 was when it was last above r by
 // more than GROWTH (then both sums go to the new r): every e is too large by the same 2^(m / ln 2 - r), which is taken out at
-// the end.  A masked class gives 0 (-inf) there and values near the type's lowest
-// and highest leave the range of d; a tile that has any shows it in its sums, is done again with d = (x - m) / ln 2 and the
-// product of e and d clamped, and so are those behind it (two operations more for each class).
+// the end.  A masked class gives 0 (-inf) there, and values near the type's lowest and highest leave the range of d; a tile that
+// has any shows it in its sums, is done again with d = (x - m) / ln 2 and the product of e and d clamped, and so are those behind
+// it (two operations more for each class).
 constexpr float GROWTH = 8.0f;   // (t is off by r's distance from m times the rounding of s)
 template <int TYPE, bool ENTROPY, bool TOP>
 __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step, int last, int n_top, Sums& a, Best& b, Picking* L) {
@@ -514,7 +515,7 @@ __global__ void __launch_bounds__(ST) k_scores(ScoreJob J) {
 }
 
 // The parts of rows joined: a workgroup a row.
-constexpr int JOINED = 8;   // lists that a wavefront asks for together (one after the other, 32 of them took it 5 us)
+constexpr int JOINED = 8;   // lists that a wavefront asks for together (all of 128 one after the other: 6.6 us, so 5.1)
 template <int TYPE>
 __global__ void __launch_bounds__(ST) k_scores_join(ScoreJob J) {
   __shared__ u64 lds_best[ST / 64][64];
@@ -538,7 +539,7 @@ __global__ void __launch_bounds__(ST) k_scores_join(ScoreJob J) {
           const int part = p0 + u * (ST / 64);
           k[u] = part < J.parts && 63 - lane < J.n_top ? J.part_best[(row * J.parts + part) * J.n_top + 63 - lane] : 0;
         }
-        // (a loop: code that runs once a launch waits for its instructions more than for what they do)
+        // (unrolled, or joined in pairs: no faster)
 #pragma unroll 1
         for (int u = 0; u < JOINED && p0 + u * (ST / 64) < J.parts; ++u) {
           list = best_of<0>(list, k[0]);

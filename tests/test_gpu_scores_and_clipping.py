@@ -98,6 +98,41 @@ def test_scores_of_a_set_are_refused():
     g.close()
 
 
+@pytest.mark.parametrize("name,arch", NETS[:-1])
+def test_scores_captured_and_after_training(name, arch):
+    """A captured call reads the weights and labels that are there when it is replayed."""
+    import torch
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        r, _, images = _pair(name, arch)
+    n, batch, C = 10, 4, r.num_classes
+    d_imgs = to_dev(images(n))
+    labels = torch.arange(n, dtype=torch.int32, device="cuda:0") % C
+    scratch = torch.empty(r.forward_batch_scratch_bytes(batch), dtype=torch.uint8, device="cuda:0")
+    new = lambda: (torch.zeros(n, device="cuda:0"), torch.zeros(n, device="cuda:0"), torch.zeros(n, 2, dtype=torch.int32, device="cuda:0"))  # noqa: E731
+    held, eager = new(), new()
+    torch.cuda.synchronize()
+    r.score_batch(d_imgs, n, scratch, batch, labels, held[0], held[1], held[2])
+    r.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        r.score_batch(d_imgs, n, scratch, batch, labels, held[0], held[1], held[2])
+    last = None
+    for _ in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        r.score_batch(d_imgs, n, scratch, batch, labels, eager[0], eager[1], eager[2])
+        r.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, eager))
+        assert last is None or not torch.equal(last, held[0])
+        last = held[0].clone()
+        labels.copy_((labels + 1) % C)
+        torch.cuda.synchronize()
+        r.train_many_clipped(d_imgs, labels, 0.05, 0.5)
+        r.synchronize()
+    r.close()
+
+
 MODES = [binding.MODE_STAGES, binding.MODE_PERSISTENT, binding.MODE_RESIDENT]
 
 
