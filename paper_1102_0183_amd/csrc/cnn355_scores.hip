@@ -466,11 +466,13 @@ __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step
   if (!rough) settle();
 }
 
+constexpr int threads_of(int waves) { return waves > ST / 64 ? waves * 64 : ST; }
+
 // Rows of more than 64 classes, WAVES wavefronts a row or, where parts > 1, a part of one.
 template <int TYPE, int WAVES, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(ST) k_scores(ScoreJob J) {
-  constexpr int ROWS = ST / 64 / WAVES;
-  __shared__ Picking lds_picking[TOP ? ST / 64 : 1];
+__global__ void __launch_bounds__(threads_of(WAVES)) k_scores(ScoreJob J) {
+  constexpr int ROWS = threads_of(WAVES) / 64 / WAVES;
+  __shared__ Picking lds_picking[TOP ? threads_of(WAVES) / 64 : 1];
   __shared__ u64 lds_best[TOP && WAVES > 1 ? WAVES : 1][64];
   __shared__ float lds_sums[WAVES][4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -491,11 +493,21 @@ __global__ void __launch_bounds__(ST) k_scores(ScoreJob J) {
       if (lane == 0) { lds_sums[w][0] = a.m; lds_sums[w][1] = a.s; lds_sums[w][2] = a.t; }
       if (TOP) lds_best[w][lane] = b.list;
       __syncthreads();
+      if (TOP && WAVES > 4) {   // two by two
+#pragma unroll 1
+        for (int half = WAVES / 2; half; half >>= 1) {
+          if (wave < half) {
+            b.list = best_of<0>(b.list, lds_best[wave + half][63 - lane]);
+            lds_best[wave][lane] = b.list;
+          }
+          __syncthreads();
+        }
+      }
       if (wave != 0) continue;
       a = Sums{LOWEST, 0.0f, 0.0f};
       if (lane < WAVES) a = Sums{lds_sums[lane][0], lds_sums[lane][1], lds_sums[lane][2]};
       join_lanes<64>(a);
-      if (TOP) {
+      if (TOP && WAVES <= 4) {
 #pragma unroll 1
         for (int o = 1; o < WAVES; ++o) b.list = best_of<0>(b.list, lds_best[o][63 - lane]);
       }
@@ -753,23 +765,28 @@ int lanes_of(int items) {   // the power of two
   return l;
 }
 
-// One wavefront a row or four: four share what is read, but each picks out its own best, and the lists have to be joined.
-// us of one / four with 20 best, bf16: 2048 rows of 8192 classes 15 / 22, 20000 91 / 186; 4096 rows of 32768 65 / 78, 1024 27 / 22;
-// of 131072 4096 rows 209 / 218, 5000 (one of two rounds a fifth full) 305 / 264.  Without best, fp32: 20000 rows of 4096 59 / 64,
-// of 8192 113 / 109, of 32768 473 / 437.
-bool one_wavefront(const ScoreJob& J) {
+// One wavefront a row, four or eight: they share what is read, but each picks out its own best, and the lists have to be joined.
+// Eight are for rows that leave compute units idle (16: no faster).
+// us of one / four with 20 best, bf16: 512 rows of 8192 classes 12.3 / 10.0, 1000 12.5 / 12.7, 2048 15 / 22, 20000 91 / 186; 4096 rows
+// of 32768 65 / 78, 1024 27 / 22; of 131072 4096 rows 209 / 218, 5000 (one of two rounds a fifth full) 305 / 264.  Without best, fp32:
+// 20000 rows of 4096 59 / 64, of 8192 113 / 109, of 32768 473 / 437.
+// us of four / eight, 20 best of bf16: one row of 8192 7.6 / 7.8, 16384 8.7 / 8.4, 32768 10.9 / 10.1, 50000 14.1 / 11.7; 250 rows of
+// 131072 26.7 / 21.8, 512 36.0 / 35.5, 600 43 / 50; one row of 50000 without best 7.7 / 5.7.
+int wavefronts_of(const ScoreJob& J) {
   const int tiles = (J.classes + SCORE_TILE - 1) / SCORE_TILE;
-  return J.parts == 1 && (tiles <= 4 || (J.n_top && (tiles <= 8 || (tiles <= 32 && J.rows >= 4096))));
+  if (J.parts > 1) return 4;
+  if (tiles <= 4 || (J.n_top && ((tiles <= 8 && J.rows > 512) || (tiles <= 32 && J.rows >= 4096)))) return 1;
+  return tiles > 8 && J.rows <= 256 ? 8 : 4;
 }
 
 template <int TYPE, int WAVES>
 hipError_t launch_scores_waves(hipStream_t stream, const ScoreJob& J) {
-  const dim3 grid(grid_of(J.rows, ST / 64 / WAVES), (unsigned)J.parts);
+  const dim3 grid(grid_of(J.rows, threads_of(WAVES) / 64 / WAVES), (unsigned)J.parts), threads(threads_of(WAVES));
   const bool h = J.entropy, top = J.n_top;
-  if (h && top) hipLaunchKernelGGL((k_scores<TYPE, WAVES, true, true>), grid, dim3(ST), 0, stream, J);
-  else if (h) hipLaunchKernelGGL((k_scores<TYPE, WAVES, true, false>), grid, dim3(ST), 0, stream, J);
-  else if (top) hipLaunchKernelGGL((k_scores<TYPE, WAVES, false, true>), grid, dim3(ST), 0, stream, J);
-  else hipLaunchKernelGGL((k_scores<TYPE, WAVES, false, false>), grid, dim3(ST), 0, stream, J);
+  if (h && top) hipLaunchKernelGGL((k_scores<TYPE, WAVES, true, true>), grid, threads, 0, stream, J);
+  else if (h) hipLaunchKernelGGL((k_scores<TYPE, WAVES, true, false>), grid, threads, 0, stream, J);
+  else if (top) hipLaunchKernelGGL((k_scores<TYPE, WAVES, false, true>), grid, threads, 0, stream, J);
+  else hipLaunchKernelGGL((k_scores<TYPE, WAVES, false, false>), grid, threads, 0, stream, J);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || J.parts == 1) return e;
   hipLaunchKernelGGL(k_scores_join<TYPE>, dim3(grid_of(J.rows, 1)), dim3(ST), 0, stream, J);
@@ -802,7 +819,11 @@ hipError_t launch_scores_type(hipStream_t stream, const ScoreJob& J) {
   if (one_by_one(J)) {
     CNN355_LANES(k_scores_rows, lanes_of((J.classes + 15) / 16))
   } else if (J.classes > 64) {
-    return one_wavefront(J) ? launch_scores_waves<TYPE, 1>(stream, J) : launch_scores_waves<TYPE, 4>(stream, J);
+    switch (wavefronts_of(J)) {
+      case 1: return launch_scores_waves<TYPE, 1>(stream, J);
+      case 4: return launch_scores_waves<TYPE, 4>(stream, J);
+      default: return launch_scores_waves<TYPE, 8>(stream, J);
+    }
   } else {
     switch (lanes_of(J.classes)) {   // (more than 8 best)
       case 16: hipLaunchKernelGGL((k_scores_few<TYPE, 16>), dim3(grid_of(J.rows, ST / 16)), dim3(ST), 0, stream, J); break;
@@ -831,13 +852,14 @@ hipError_t launch_scores_grad_type(hipStream_t stream, const ScoreGradJob& J) {
 
 // How rows are shared where there are too few of them to fill the chip: parts of eight tiles or more, for two workgroups a compute
 // unit at most; they cost a second launch that waits for the first.  us in parts / by one workgroup a row, 20 best of bf16: one row
-// of 16384 classes 13.7 / 9.8, 32768 13.3 / 12.1, 50000 13.7 / 15.4; 300 rows of 32768 17.9 / 14.9.  Without best one row of 50000
-// takes 13.6 / 9.1, one of 97000 13.5 / 13.0.  Parts of four tiles: one row of 8192 12.5 (one workgroup 10.8), 64 of 131072 17.3 (eight 16.9).
+// of 50000 classes 14.1 / 12.6, 65536 13.7 / 12.6, 80000 14.1 / 15.1, 131072 14.2 / 18.5, 1000000 20.6 / 86; of 131072 64 rows 17.0 / 19.5,
+// 110 19.1 / 19.6, 180 23.6 / 20.9, 250 25.7 / 21.7.  Without best one row of 50000 takes 9.6 / 8.9, 131072 of fp32 13.1 / 10.9, of bf16
+// 22.3 / 25.0 (with the wait for it), 200000 22.3 / 29.0.  Parts of 16 tiles by eight wavefronts: one row of 131072 13.9, 64 17.2.
 void score_parts(long long rows, int classes, int n_top, int* parts, int* part_tiles) {
   const int tiles = (classes + SCORE_TILE - 1) / SCORE_TILE;
   *parts = 1;
   *part_tiles = tiles;
-  if (rows >= 512 || tiles <= (n_top ? 40 : 80)) return;
+  if (rows >= 128 || tiles <= (n_top ? 64 : 100)) return;
   const long long want = std::min<long long>({(512 + rows - 1) / rows, (tiles + 7) / 8, SCORE_PARTS});
   *part_tiles = (int)((tiles + want * 4 - 1) / (want * 4)) * 4;
   *parts = (tiles + *part_tiles - 1) / *part_tiles;

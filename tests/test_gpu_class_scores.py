@@ -54,10 +54,11 @@ def _call(x, labels, top, want=("lp", "h", "norm", "top", "top_lp"), stream=None
 
 
 def _terms(rows, n):
-    """Terms that one lane adds at most: one wavefront a row up to 8192 classes, and one more tile where a row starts oddly."""
+    """Terms that one lane adds at most: one wavefront a row up to 8192 classes, or 32768 of many rows, else four or more, and one more
+    tile where a row starts oddly."""
     if n <= 64:
         return 1
-    return 16 * (math.ceil(math.ceil(n / 1024) / (1 if n <= 8192 else 4)) + 1)
+    return 16 * (math.ceil(math.ceil(n / 1024) / (1 if n <= 8192 or (rows >= 4096 and n <= 32768) else 4)) + 1)
 
 
 def _check(x, labels, top, out):
@@ -170,6 +171,22 @@ def test_many_rows(rows, n, top, dtype):
     x[rows // 3, 1:] = -math.inf
     x[rows // 2, 3] = math.nan
     _sampled(x, labels, top, _call(x, labels, top), [0, 1, rows // 3, rows // 2, rows - 2, rows - 1] + list(range(5, rows, rows // 9)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n,top", [(1, 9217, 64), (2, 8192, 64), (5, 65536, 20), (3, 65537, 20), (37, 50003, 25), (128, 66001, 20), (127, 66001, 20),
+                                        (200, 100003, 64), (256, 30011, 8), (257, 30011, 8), (40, 102401, 0), (1, 102399, 0), (512, 8000, 5), (513, 8000, 5)])
+def test_few_long_rows(rows, n, top, dtype):
+    """Rows that one, four or eight wavefronts share, and parts of them, on both sides of the rules' edges."""
+    x, labels = _rows(rows, n, dtype, n + rows, pad=n % 3)
+    at = sorted({0, rows - 1, rows // 3, rows // 2})
+    if rows > 4:
+        x[rows // 3, 1:] = -math.inf
+        x[rows // 2, n - 1] = math.nan
+        x[1, ::2] = -math.inf
+        x[2] = x[2, 0].item()
+        at = sorted(set(at) | {1, 2, rows - 2})
+    _sampled(x, labels, top, _call(x, labels, top), at)
 
 
 @pytest.mark.parametrize("rows,n,top,dtype", [
