@@ -39,15 +39,39 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // ---- keys of values: u64 order is (value, lower index first); 0 is below every key ----
+// A key is a double above zero, whose order is the same: 63 bits, and the exponent of +inf's key is 0x7fc.
 __device__ __forceinline__ u64 key_of(float v, int index) {
   const unsigned b = __builtin_bit_cast(unsigned, v + 0.0f);   // (-0 as 0)
-  return (u64)((int)b < 0 ? ~b : b | 0x80000000u) << 32 | (unsigned)~index;
+  return (u64)((int)b < 0 ? ~b : b | 0x80000000u) << 31 | (~index & 0x7fffffff);
 }
 __device__ __forceinline__ u64 key_of_any(float v, int index) { return v == v ? key_of(v, index) : 0; }   // (0: no number)
-__device__ __forceinline__ int index_of(u64 k) { return (int)~(unsigned)k; }
+__device__ __forceinline__ int index_of(u64 k) { return ~(int)k & 0x7fffffff; }
 __device__ __forceinline__ float value_of(u64 k) {
-  const unsigned b = (unsigned)(k >> 32);
+  const unsigned b = (unsigned)(k >> 31);
   return __builtin_bit_cast(float, (int)b < 0 ? b & 0x7fffffffu : ~b);
+}
+__device__ __forceinline__ u64 above_value_of(u64 k) { return k + (1ull << 31); }
+
+// a float's order as a whole number's, and back
+__device__ __forceinline__ int order_of(float v) {
+  const int b = __builtin_bit_cast(int, v);
+  return b ^ (b >> 31 & 0x7fffffff);
+}
+__device__ __forceinline__ float of_order(int o) { return __builtin_bit_cast(float, o ^ (o >> 31 & 0x7fffffff)); }
+
+__device__ __forceinline__ int larger_of(int a, int b) { return a > b ? a : b; }
+__device__ __forceinline__ int smaller_of(int a, int b) { return a < b ? a : b; }
+// keys as doubles: an operation each (compared as whole numbers, whose outcome goes through the scalar unit, 37 rows of 100003
+// classes took 16.1 us, so 15.0, one row of 50000 12.4, so 11.8)
+__device__ __forceinline__ u64 larger_of(u64 a, u64 b) {
+  double r;
+  asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(__builtin_bit_cast(double, a)), "v"(__builtin_bit_cast(double, b)));
+  return __builtin_bit_cast(u64, r);
+}
+__device__ __forceinline__ u64 smaller_of(u64 a, u64 b) {
+  double r;
+  asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(__builtin_bit_cast(double, a)), "v"(__builtin_bit_cast(double, b)));
+  return __builtin_bit_cast(u64, r);
 }
 
 // ---- between lanes, without LDS ----
@@ -69,6 +93,8 @@ __device__ __forceinline__ unsigned xor_word(unsigned v) {
 }
 template <int D>
 __device__ __forceinline__ float xor_lane(float v) { return __builtin_bit_cast(float, xor_word<D>(__builtin_bit_cast(unsigned, v))); }
+template <int D>
+__device__ __forceinline__ int xor_lane(int v) { return (int)xor_word<D>((unsigned)v); }
 template <int D>
 __device__ __forceinline__ u64 xor_lane(u64 v) { return (u64)xor_word<D>((unsigned)(v >> 32)) << 32 | xor_word<D>((unsigned)v); }
 
@@ -119,8 +145,8 @@ __device__ __forceinline__ T merge_lanes(T v) {
     const bool rises = RISE == 64 || (lane & RISE) != 0, larger = ((lane & D) == 0) != rises;
     T a, b;
     pair_of<D>(v, a, b);
-    v = (a < b) == larger ? b : a;   // (equal ones: either)
-    return merge_lanes<D / 2, RISE>(v);
+    const T most = larger_of(a, b), least = smaller_of(a, b);
+    return merge_lanes<D / 2, RISE>(larger ? most : least);
   } else {
     return v;
   }
@@ -133,7 +159,7 @@ __device__ __forceinline__ T sort_lanes(T v) {
 }
 // the larger ones of two sorted runs of 64, the first falling and the second rising; sorted
 template <int RISE, class T>
-__device__ __forceinline__ T best_of(T falling, T rising) { return merge_lanes<32, RISE>(falling < rising ? rising : falling); }
+__device__ __forceinline__ T best_of(T falling, T rising) { return merge_lanes<32, RISE>(larger_of(falling, rising)); }
 
 // ---- sums of a row ----
 struct Sums {
@@ -249,9 +275,7 @@ struct Best {
 __device__ __forceinline__ u64 lane_of(u64 v, int lane) {
   return (u64)__builtin_amdgcn_readlane((unsigned)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((unsigned)v, lane);
 }
-__device__ __forceinline__ float lane_of(float v, int lane) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
-}
+__device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 __device__ __forceinline__ int place_in(u64 lanes) { return __builtin_amdgcn_mbcnt_hi((unsigned)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)lanes, 0)); }
 __device__ __forceinline__ void lds_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }   // (a wavefront's own lanes)
 
@@ -268,7 +292,7 @@ __device__ __forceinline__ void take_held(Best& b, Picking& L, int n_top) {
   if (last > b.bar) {
     // (the classes of the tiles to come have higher indices: of theirs, only larger values are above that key)
     b.bar = last;
-    b.bar_value = value_of(last + (1ull << 32));
+    b.bar_value = value_of(above_value_of(last));
   }
 }
 
@@ -300,7 +324,8 @@ __device__ __forceinline__ void pick(Best& b, Picking& L, const RowAt<TYPE>& row
   typedef Element<TYPE> E;
   constexpr int V = E::V;
   const int lane = threadIdx.x & 63;
-  const float v = lane_of(n_top <= 24 ? sort_lanes<64, 0>(fmaxf(m0, m1)) : best_of<0>(sort_lanes<64, 0>(m0), sort_lanes<64, 64>(m1)), n_top - 1);
+  const int o0 = order_of(m0), o1 = order_of(m1);
+  const float v = of_order(lane_of(n_top <= 24 ? sort_lanes<64, 0>(larger_of(o0, o1)) : best_of<0>(sort_lanes<64, 0>(o0), sort_lanes<64, 64>(o1)), n_top - 1));
   if (v > b.bar_value) {
     b.bar_value = v;
     b.bar = key_of(v, -1);
