@@ -163,7 +163,7 @@ def _know_torch():
     global _kinds, _f32, _i32, _u8, _current_device, _raw_stream, _device_guard
     import torch
     _f32, _i32, _u8 = torch.float32, torch.int32, torch.uint8
-    _current_device, _device_guard = torch.cuda.current_device, torch.cuda.device
+    _current_device, _device_guard = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device, torch.cuda.device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
     _kinds = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
 
@@ -172,43 +172,41 @@ def _element_type(t):
     """TYPE_* of a tensor."""
     if not _kinds:
         _know_torch()
-    assert t.dtype in _kinds, "expected float32, bfloat16 or float16"
-    return _kinds[t.dtype]
+    kind = _kinds.get(t.dtype)
+    assert kind is not None, "expected float32, bfloat16 or float16"
+    return kind
 
 
 def _address(t, kind, shape, device):
-    """Address of a contiguous tensor of this type and shape (None: None)."""
+    """Address of a contiguous tensor of this type and shape on a device, given by its number (None: None)."""
     if t is None:
         return None
-    assert t.dtype == kind and t.shape == shape and t.device == device and t.is_contiguous(), \
-        "expected a contiguous %s tensor %r on %s" % (kind, tuple(shape), device)
+    assert t.dtype is kind and t.get_device() == device and t.shape == shape and t.is_contiguous(), \
+        "expected a contiguous %s tensor %r on device %d" % (kind, tuple(shape), device)
     return t.data_ptr()
 
 
 def _rows_of(t):
-    """(address, type, rows, classes, elements between rows) of a matrix whose rows are contiguous."""
-    kind = _element_type(t)
-    assert t.is_cuda and t.dim() == 2, "expected a device matrix"
-    rows, classes = t.shape
+    """(address, type, rows, classes, elements between rows, device number) of a matrix whose rows are contiguous."""
+    kind, shape, device = _element_type(t), t.shape, t.get_device()
+    assert device >= 0 and len(shape) == 2, "expected a device matrix"
+    rows, classes = shape
     stride, across = t.stride()
     assert classes <= 1 or across == 1, "the elements of a row must lie side by side"
-    return t.data_ptr(), kind, rows, classes, max(stride, classes) if rows <= 1 else stride
+    return t.data_ptr(), kind, rows, classes, max(stride, classes) if rows <= 1 else stride, device
 
 
 def _scratch_of(t, device):
     if t is None or t.numel() == 0:
         return None, 0
-    assert t.dtype == _u8 and t.device == device and t.is_contiguous()
+    assert t.dtype is _u8 and t.get_device() == device and t.is_contiguous(), "expected contiguous uint8 scratch memory on device %d" % device
     return t.data_ptr(), t.numel()
 
 
 def _on(device, stream, call, *args):
     """call(stream, *args) with the device of its tensors the current one."""
-    if stream is not None:
-        raw = stream.cuda_stream
-    else:
-        raw = _raw_stream(device.index)
-    if _current_device() == device.index:
+    raw = _raw_stream(device) if stream is None else stream.cuda_stream
+    if _current_device() == device:
         return call(raw, *args)
     with _device_guard(device):
         return call(raw, *args)
@@ -229,8 +227,7 @@ def class_scores(d_logits, d_labels=None, d_log_probs=None, d_entropy=None, d_no
     outputs (each of them or None) float32 d_log_probs [rows], d_entropy [rows], d_normaliser [rows][2], int32 d_top and
     float32 d_top_log_probs [rows][n_top]; d_scratch: uint8, class_scores_scratch_bytes(rows, classes, n_top) of it.
     Asynchronous on `stream` (a torch stream; None: the current)."""
-    x, kind, rows, classes, stride = _rows_of(d_logits)
-    dev = d_logits.device
+    x, kind, rows, classes, stride, dev = _rows_of(d_logits)
     some = d_top if d_top is not None else d_top_log_probs
     n_top = 0 if some is None else some.shape[-1]
     scratch, nbytes = _scratch_of(d_scratch, dev)
@@ -245,10 +242,10 @@ def class_scores(d_logits, d_labels=None, d_log_probs=None, d_entropy=None, d_no
 def class_scores_grad(d_logits, d_grad, d_normaliser, d_labels=None, d_g_log_probs=None, d_entropy=None, d_g_entropy=None, stream=None):
     """cnn_class_scores_grad: d_grad, of d_logits' shape and type (or d_logits itself), receives the gradient of
     sum(d_g_log_probs * log_probs) + sum(d_g_entropy * entropy); d_normaliser and d_entropy as class_scores gave them."""
-    x, kind, rows, classes, stride = _rows_of(d_logits)
-    g, g_kind, g_rows, g_classes, g_stride = _rows_of(d_grad)
-    dev, each = d_logits.device, (rows,)
-    assert d_grad.device == dev and (g_kind, g_rows, g_classes) == (kind, rows, classes)
+    x, kind, rows, classes, stride, dev = _rows_of(d_logits)
+    g, g_kind, g_rows, g_classes, g_stride, g_dev = _rows_of(d_grad)
+    each = (rows,)
+    assert g_dev == dev and g_kind == kind and g_rows == rows and g_classes == classes, "expected a gradient of the rows' type, shape and device"
     rc = _on(dev, stream, lib().cnn_class_scores_grad, x, kind, rows, classes, stride, _address(d_labels, _i32, each, dev),
              _address(d_normaliser, _f32, (rows, 2), dev), _address(d_entropy, _f32, each, dev), _address(d_g_log_probs, _f32, each, dev),
              _address(d_g_entropy, _f32, each, dev), g, g_stride)
@@ -304,18 +301,19 @@ def gradient_scratch_bytes(n):
 
 
 def _over_gradients(grads, other, d_norm, d_scratch):
-    """(device, address of the norm, scratch, its bytes) of a call, its lists looked over."""
+    """(device number, address of the norm, scratch, its bytes) of a call, its lists looked over."""
     if _f32 is None:
         _know_torch()
-    dev = grads.device
-    if dev is None:
+    if grads.device is not None:
+        dev = grads.device.index
+    else:
         some = d_norm if d_norm is not None else d_scratch
-        assert some is not None, "expected scratch memory"
-        dev = some.device
+        assert some is not None and some.is_cuda, "expected scratch memory"
+        dev = some.get_device()
     if other is not None:
         assert len(other) == len(grads) and other.device == grads.device and other.orders == grads.orders, \
             "lists that go together have the same tensors, laid out alike"
-    assert d_norm is None or (d_norm.dtype == _f32 and d_norm.numel() == 1 and d_norm.device == dev)
+    assert d_norm is None or (d_norm.dtype is _f32 and d_norm.numel() == 1 and d_norm.get_device() == dev), "expected a norm of one float32"
     return (dev, None if d_norm is None else d_norm.data_ptr()) + _scratch_of(d_scratch, dev)
 
 
@@ -632,8 +630,8 @@ class Cnn:
         torch = self._torch
         if _f32 is None:
             _know_torch()
-        dev = d_images.device
-        assert dev == self.workspace.device and d_images.dtype == torch.float32 and d_images.is_contiguous()
+        dev = d_images.get_device()
+        assert dev == self.workspace.get_device() and d_images.dtype == torch.float32 and d_images.is_contiguous()
         assert d_images.numel() >= n * self.image_size
         scratch, nbytes = _scratch_of(d_scratch, dev)
         some = d_top if d_top is not None else d_top_log_probs
