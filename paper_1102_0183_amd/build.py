@@ -14,7 +14,7 @@ SOURCES = ["cnn355_kernels.hip", "cnn355_winners.hip", "cnn355_flow.hip", "cnn35
            "cnn355_gradients.hip", "cnn355_api.hip"]
 HEADERS = [os.path.join(CSRC, "cnn355_dev.h"), os.path.join(CSRC, "cnn355_flowspec.h"),
            os.path.join(CSRC, "cnn355_stage.h"), os.path.join(CSRC, "cnn355_first.h"), os.path.join(CSRC, "cnn355_winners.h"),
-           os.path.join(CSRC, "cnn355_ops.h"), os.path.join(CSRC, "cnn355_elements.h"),
+           os.path.join(CSRC, "cnn355_ops.h"), os.path.join(CSRC, "cnn355_elements.h"), os.path.join(CSRC, "cnn355_lanes.h"),
            os.path.join(HERE, "..", "include", "cnn355.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-FP32 instructions are switched off on purpose: some of their forms have given wrong

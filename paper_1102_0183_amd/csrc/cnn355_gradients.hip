@@ -15,6 +15,7 @@
 #define CNN_GLOBAL __attribute__((address_space(1)))
 #include "cnn355_ops.h"
 #include "cnn355_elements.h"
+#include "cnn355_lanes.h"
 
 namespace cnn355 {
 
@@ -27,10 +28,15 @@ typedef unsigned v2u_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
 
+template <int D>
+__device__ __forceinline__ double add_lane(double s) {   // and that of the lane whose number differs by D
+  const unsigned long long b = __builtin_bit_cast(unsigned long long, s);
+  return s + __builtin_bit_cast(double, (unsigned long long)xor_word<D>((unsigned)(b >> 32)) << 32 | xor_word<D>((unsigned)b));
+}
 // the sum of a double of every thread, in every thread
 template <int THREADS>
 __device__ __forceinline__ double sum_of_workgroup(double s, double* lds) {
-  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  s = add_lane<1>(add_lane<2>(add_lane<4>(add_lane<8>(add_lane<16>(add_lane<32>(s))))));
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) lds[wave] = s;
   __syncthreads();
@@ -91,8 +97,10 @@ __device__ __forceinline__ Share share_of_workgroup() { return Share{blockIdx.x,
 // one is looked up while the loads of a chunk are under way (its loads too: no faster, and clipping of 320 tensors 288 us -> 304).
 // FOURS: types of 16 bits in loads of 8 bytes, two in the place of one of 16, so that the fp32 values that belong to a wavefront's
 // load lie side by side too.
-template <bool FAR, bool DOWN, bool FOURS, class JOB, class Full, class Part>
-__device__ __forceinline__ void for_chunks(const JOB& J, Share at, Full full, Part part) {
+// early(piece): what else a whole chunk wants loaded; goes_on(): called behind the loads of every chunk, with whole workgroups, so that
+// what has to be known first (a norm) is waited for together with them; the loop ends where it says no.
+template <bool FAR, bool DOWN, bool FOURS, class JOB, class Early, class GoesOn, class Full, class Part>
+__device__ __forceinline__ void for_chunks(const JOB& J, Share at, Early early, GoesOn goes_on, Full full, Part part) {
   int t = DOWN ? J.tensors - 1 : 0;
   Piece p = piece_of<FAR, DOWN>(J, at.first, t);
   for (unsigned i = at.first; i < J.chunks; i += at.step) {
@@ -110,10 +118,13 @@ __device__ __forceinline__ void for_chunks(const JOB& J, Share at, Full full, Pa
 #pragma unroll
         for (int q = 0; q < NV; ++q) r[q] = *(const CNN_GLOBAL v4u_any*)(p.from + (q * GT + at.thread) * 16);
       }
+      early(p);
       next = piece_of<FAR, DOWN>(J, i + at.step, t);
+      if (!goes_on()) return;
       full(p, r);
     } else {
       next = piece_of<FAR, DOWN>(J, i + at.step, t);
+      if (!goes_on()) return;
       part(p);
     }
     p = next;
@@ -135,7 +146,7 @@ template <bool FAR, class JOB>
 __device__ __forceinline__ double squares_of(const JOB& J, Share at) {
   double s = 0.0;
   for_chunks<FAR, false, false>(
-      J, at,
+      J, at, [](const Piece&) {}, []() { return true; },
       [&](const Piece& p, const v4u (&r)[NV]) {
         by_type(p.type, [&](auto type) {
           typedef Element<decltype(type)::value> E;
@@ -176,15 +187,26 @@ __global__ void __launch_bounds__(128) k_table(TensorJob J, CNN_GLOBAL TensorEnt
   o->from = e.from; o->to = e.to; o->n = e.n; o->chunk = e.chunk; o->type = e.type;
 }
 
-__device__ __forceinline__ double norm_of(const CNN_GLOBAL double* sums, int n, double* lds) {
+// the sums, asked for, and the root of what they come to
+struct Sums {
+  double v[LIST_SUMS / GT];
+};
+__device__ __forceinline__ Sums load_sums(const CNN_GLOBAL double* sums, int n) {
+  Sums r;
+#pragma unroll
+  for (int k = 0; k < LIST_SUMS / GT; ++k) r.v[k] = (int)threadIdx.x + k * GT < n ? sums[threadIdx.x + k * GT] : 0.0;
+  return r;
+}
+__device__ __forceinline__ double norm_of(const Sums& sums, double* lds) {
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += GT) s += sums[i];
+#pragma unroll
+  for (int k = 0; k < LIST_SUMS / GT; ++k) s += sums.v[k];
   return sqrt(sum_of_workgroup<GT>(s, lds));
 }
 
 __global__ void __launch_bounds__(GT) k_norm(const CNN_GLOBAL double* sums, int n, CNN_GLOBAL float* norm) {
   __shared__ double lds[GT / 64];
-  const double v = norm_of(sums, n, lds);
+  const double v = norm_of(load_sums(sums, n), lds);
   if (threadIdx.x == 0) *norm = (float)v;
 }
 
@@ -220,15 +242,24 @@ __device__ __forceinline__ v4u times(v4u r, const Factor& f) {
   return v;
 }
 
-// to = f g of a share's chunks, f = max_norm / v where that is less than 1; to may be the gradients themselves (in_place: all are)
-template <bool FAR, class JOB>
-__device__ __forceinline__ void scale(const JOB& J, Share at, double v, double max_norm, int in_place) {
-  const bool clips = v < __builtin_inf() && v > max_norm;
-  if (!clips && in_place) return;
-  const Factor f = factor_of(clips ? max_norm / v : 1.0);
+// to = f g of a share's chunks, f = max_norm / v where that is less than 1; to may be the gradients themselves (in_place: all are).
+// norm(): v
+template <bool FAR, class JOB, class Norm>
+__device__ __forceinline__ void scale(const JOB& J, Share at, Norm norm, double max_norm, int in_place) {
+  bool known = false, clips = false;
+  Factor f;
+  auto goes_on = [&]() {
+    if (!known) {
+      const double v = norm();
+      clips = v < __builtin_inf() && v > max_norm;
+      f = factor_of(clips ? max_norm / v : 1.0);
+      known = true;
+    }
+    return clips || !in_place;
+  };
   // the last chunks first: they are the ones that the launch before read last, and may still be in a cache
   for_chunks<FAR, true, false>(
-      J, at,
+      J, at, [](const Piece&) {}, goes_on,
       [&](const Piece& p, const v4u (&r)[NV]) {
         by_type(p.type, [&](auto type) {
           constexpr int TYPE = decltype(type)::value;
@@ -252,40 +283,48 @@ __device__ __forceinline__ void scale(const JOB& J, Share at, double v, double m
           if (last < p.n) o[last] = clips ? times<TYPE>(Element<TYPE>::get(g[last]), f) : g[last];
         });
       });
+  if (!known) goes_on();
 }
 
-// to (weights) -= lr f g
-template <bool FAR, class JOB>
-__device__ __forceinline__ void update(const JOB& J, Share at, double v, double max_norm, double lr) {
-  if (!(v < __builtin_inf())) return;
-  const double f = -lr * (v > max_norm ? max_norm / v : 1.0);
+// to (weights) -= lr f g; norm(): v
+template <bool FAR, class JOB, class Norm>
+__device__ __forceinline__ void update(const JOB& J, Share at, Norm norm, double max_norm, double lr) {
+  bool known = false, finite = false;
+  double f = 0.0;
+  auto goes_on = [&]() {
+    if (!known) {
+      const double v = norm();
+      finite = v < __builtin_inf();
+      f = -lr * (v > max_norm ? max_norm / v : 1.0);
+      known = true;
+    }
+    return finite;
+  };
   auto one = [&](float w, float g) { return (float)fma(f, (double)g, (double)w); };
+  v4f o[2 * NV];
   for_chunks<FAR, true, true>(
       J, at,
+      [&](const Piece& p) {
+        const CNN_GLOBAL float* w = (const CNN_GLOBAL float*)p.to + p.begin;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
+        if (p.type != ELEMENT_F32) {
+#pragma unroll
+          for (int q = NV; q < 2 * NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
+        }
+      },
+      goes_on,
       [&](const Piece& p, const v4u (&r)[NV]) {
         by_type(p.type, [&](auto type) {
           typedef Element<decltype(type)::value> E;
           CNN_GLOBAL float* w = (CNN_GLOBAL float*)p.to + p.begin;
-          if constexpr (E::V == 4) {
-            v4f o[NV];
+          constexpr int N = E::V == 4 ? NV : 2 * NV;
 #pragma unroll
-            for (int q = 0; q < NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
+          for (int q = 0; q < N; ++q) {
+            v4f v = o[q];
 #pragma unroll
-            for (int q = 0; q < NV; ++q) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) o[q][j] = one(o[q][j], E::get(r[q], j));
-              __builtin_nontemporal_store(o[q], (CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
-            }
-          } else {
-            v4f o[2 * NV];
-#pragma unroll
-            for (int q = 0; q < 2 * NV; ++q) o[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
-#pragma unroll
-            for (int q = 0; q < 2 * NV; ++q) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) o[q][j] = one(o[q][j], E::get(r[q >> 1], (q & 1) * 4 + j));
-              __builtin_nontemporal_store(o[q], (CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
-            }
+            for (int j = 0; j < 4; ++j) v[j] = one(v[j], E::V == 4 ? E::get(r[q], j) : E::get(r[q >> 1], (q & 1) * 4 + j));
+            __builtin_nontemporal_store(v, (CNN_GLOBAL v4f_any*)(w + (q * GT + at.thread) * 4));
           }
         });
       },
@@ -297,6 +336,13 @@ __device__ __forceinline__ void update(const JOB& J, Share at, double v, double 
           for (int i = at.thread; i < p.n; i += GT) w[i] = one(w[i], E::get(g[i]));
         });
       });
+  if (!known) goes_on();
+}
+
+// v, and where it is wanted
+__device__ __forceinline__ double give_norm(double v, CNN_GLOBAL float* norm) {
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+  return v;
 }
 
 // Whether the gradients are of an image that is passed over for its label (its norm is 0)
@@ -309,18 +355,16 @@ __device__ __forceinline__ bool passed_over(const TensorHead& J, CNN_GLOBAL floa
 template <class JOB, bool FAR>
 __global__ void __launch_bounds__(GT) k_scale(JOB J, const CNN_GLOBAL double* sums, double max_norm, CNN_GLOBAL float* norm, int in_place) {
   __shared__ double lds[GT / 64];
-  const double v = norm_of(sums, J.sums, lds);
-  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
-  scale<FAR>(J, share_of_workgroup(), v, max_norm, in_place);
+  const Sums all = load_sums(sums, J.sums);
+  scale<FAR>(J, share_of_workgroup(), [&]() { return give_norm(norm_of(all, lds), norm); }, max_norm, in_place);
 }
 
 template <class JOB, bool FAR>
 __global__ void __launch_bounds__(GT) k_update(JOB J, const CNN_GLOBAL double* sums, double max_norm, double lr, CNN_GLOBAL float* norm) {
   __shared__ double lds[GT / 64];
   if (passed_over(J, norm)) return;
-  const double v = norm_of(sums, J.sums, lds);
-  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
-  update<FAR>(J, share_of_workgroup(), v, max_norm, lr);
+  const Sums all = load_sums(sums, J.sums);
+  update<FAR>(J, share_of_workgroup(), [&]() { return give_norm(norm_of(all, lds), norm); }, max_norm, lr);
 }
 
 // Small lists in one launch: every workgroup, four groups of GT threads, adds the squares of all chunks for itself (the same way, so
@@ -333,11 +377,10 @@ __global__ void __launch_bounds__(GT * SMALL_GROUPS) k_small(JOB J, double max_n
   if (passed_over(J, norm)) return;
   const unsigned group = __builtin_amdgcn_readfirstlane(threadIdx.x / GT);
   const int thread = threadIdx.x % GT;
-  const double v = sqrt(sum_of_workgroup<GT * SMALL_GROUPS>(squares_of<false>(J, Share{group, SMALL_GROUPS, thread}), lds));
-  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
+  const double v = give_norm(sqrt(sum_of_workgroup<GT * SMALL_GROUPS>(squares_of<false>(J, Share{group, SMALL_GROUPS, thread}), lds)), norm);
   const Share own = {blockIdx.x * SMALL_GROUPS + group, gridDim.x * SMALL_GROUPS, thread};
-  if (OP == 1) scale<false>(J, own, v, max_norm, 0);
-  if (OP == 2) update<false>(J, own, v, max_norm, lr);
+  if (OP == 1) scale<false>(J, own, [&]() { return v; }, max_norm, 0);
+  if (OP == 2) update<false>(J, own, [&]() { return v; }, max_norm, lr);
 }
 
 constexpr unsigned APPLY_GRID = 2048;

@@ -20,6 +20,7 @@
 #define CNN_GLOBAL __attribute__((address_space(1)))
 #include "cnn355_ops.h"
 #include "cnn355_elements.h"
+#include "cnn355_lanes.h"
 
 namespace cnn355 {
 
@@ -75,22 +76,6 @@ __device__ __forceinline__ u64 smaller_of(u64 a, u64 b) {
 }
 
 // ---- between lanes, without LDS ----
-// a word of the lane whose number differs by D (a power of two)
-template <int D>
-__device__ __forceinline__ unsigned xor_word(unsigned v) {
-  if constexpr (D == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true);        // quad_perm [1, 0, 3, 2]
-  else if constexpr (D == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true);   // quad_perm [2, 3, 0, 1]
-  else if constexpr (D == 4)                                                             // row_half_mirror, quad_perm [3, 2, 1, 0]
-    return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true), 0x1B, 0xf, 0xf, true);
-  else if constexpr (D == 8) return __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true);  // row_ror:8
-  else if constexpr (D == 16) {
-    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    return threadIdx.x & 16 ? r[0] : r[1];
-  } else {
-    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    return threadIdx.x & 32 ? r[0] : r[1];
-  }
-}
 template <int D>
 __device__ __forceinline__ float xor_lane(float v) { return __builtin_bit_cast(float, xor_word<D>(__builtin_bit_cast(unsigned, v))); }
 template <int D>
