@@ -333,7 +333,41 @@ __device__ __forceinline__ void update(const JOB& J, Share at, Norm norm, double
           typedef Element<decltype(type)::value> E;
           const CNN_GLOBAL typename E::T* g = (const CNN_GLOBAL typename E::T*)p.from;
           CNN_GLOBAL float* w = (CNN_GLOBAL float*)p.to + p.begin;
-          for (int i = at.thread; i < p.n; i += GT) w[i] = one(w[i], E::get(g[i]));
+          const int fours = p.n >> 2, rest = (p.n & ~3) + at.thread;
+          float w_rest = 0.0f, g_rest = 0.0f;
+          if (rest < p.n) {
+            w_rest = w[rest];
+            g_rest = E::get(g[rest]);
+          }
+#pragma unroll 1
+          for (int i0 = at.thread; i0 < fours; i0 += NV * GT) {   // (a float at a time, the widest colour net took 17.3 us in fp16, so 12.6)
+            v4f u[NV];
+            v4u r[NV];
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+              u[q] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+              r[q] = v4u{0, 0, 0, 0};
+              const int i = i0 + q * GT;
+              if (i >= fours) continue;
+              u[q] = __builtin_nontemporal_load((const CNN_GLOBAL v4f_any*)(w + i * 4));
+              if constexpr (E::V == 4) {
+                r[q] = *(const CNN_GLOBAL v4u_any*)(g + i * 4);
+              } else {
+                const v2u v = *(const CNN_GLOBAL v2u_any*)(g + i * 4);
+                r[q][0] = v[0];
+                r[q][1] = v[1];
+              }
+            }
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+              const int i = i0 + q * GT;
+              if (i >= fours) continue;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) u[q][j] = one(u[q][j], E::get(r[q], j));
+              __builtin_nontemporal_store(u[q], (CNN_GLOBAL v4f_any*)(w + i * 4));
+            }
+          }
+          if (rest < p.n) w[rest] = one(w_rest, g_rest);
         });
       });
   if (!known) goes_on();
