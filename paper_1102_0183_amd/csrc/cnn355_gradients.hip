@@ -276,11 +276,19 @@ __device__ __forceinline__ void scale(const JOB& J, Share at, Norm norm, double 
           const CNN_GLOBAL T* g = (const CNN_GLOBAL T*)p.from;
           CNN_GLOBAL T* o = (CNN_GLOBAL T*)p.to + p.begin;
           const int n = p.n / V, last = n * V + at.thread;
-          for (int i = at.thread; i < n; i += GT) {
-            const v4u r = *(const CNN_GLOBAL v4u_any*)(g + i * V);
-            *(CNN_GLOBAL v4u_any*)(o + i * V) = clips ? times<TYPE>(r, f) : r;
+          T rest = {};
+          if (last < p.n) rest = g[last];
+          v4u r[NV];
+#pragma unroll
+          for (int q = 0; q < NV; ++q) {
+            r[q] = v4u{0, 0, 0, 0};
+            if (q * GT + at.thread < n) r[q] = *(const CNN_GLOBAL v4u_any*)(g + (q * GT + at.thread) * V);
           }
-          if (last < p.n) o[last] = clips ? times<TYPE>(Element<TYPE>::get(g[last]), f) : g[last];
+#pragma unroll
+          for (int q = 0; q < NV; ++q)
+            if (q * GT + at.thread < n)
+              __builtin_nontemporal_store(clips ? times<TYPE>(r[q], f) : r[q], (CNN_GLOBAL v4u_any*)(o + (q * GT + at.thread) * V));
+          if (last < p.n) o[last] = clips ? times<TYPE>(Element<TYPE>::get(rest), f) : rest;
         });
       });
   if (!known) goes_on();
