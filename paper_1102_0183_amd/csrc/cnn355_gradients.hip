@@ -161,12 +161,22 @@ __device__ __forceinline__ double squares_of(const JOB& J, Share at) {
           typedef Element<decltype(type)::value> E;
           const CNN_GLOBAL typename E::T* g = (const CNN_GLOBAL typename E::T*)p.from;
           const int n = p.n / E::V, last = n * E::V + at.thread;
-          for (int i = at.thread; i < n; i += GT) {
-            const v4u r = *(const CNN_GLOBAL v4u_any*)(g + i * E::V);
+          float rest = 0.0f;
+          if (last < p.n) rest = E::get(g[last]);
+          v4u r[NV];
 #pragma unroll
-            for (int j = 0; j < E::V; ++j) { const double v = E::get(r, j); s = fma(v, v, s); }
+          for (int q = 0; q < NV; ++q) {
+            if (q * GT >= n) break;
+            r[q] = v4u{0, 0, 0, 0};
+            if (q * GT + at.thread < n) r[q] = *(const CNN_GLOBAL v4u_any*)(g + (q * GT + at.thread) * E::V);
           }
-          if (last < p.n) { const double v = E::get(g[last]); s = fma(v, v, s); }
+#pragma unroll
+          for (int q = 0; q < NV; ++q) {
+            if (q * GT >= n) break;
+#pragma unroll
+            for (int j = 0; j < E::V; ++j) { const double v = E::get(r[q], j); s = fma(v, v, s); }
+          }
+          s = fma((double)rest, (double)rest, s);
         });
       });
   return s;
