@@ -70,6 +70,7 @@ struct TensorHead {
 };
 template <int N>
 struct TensorsOf : TensorHead {
+  static constexpr int MOST = N;
   TensorEntry e[N];
 };
 typedef TensorsOf<LIST_MOST> TensorJob;
