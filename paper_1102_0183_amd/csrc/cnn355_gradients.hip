@@ -512,7 +512,21 @@ hipError_t launch_squares(hipStream_t stream, const TensorJob& J, double* sums) 
   });
 }
 
-bool list_is_small(const TensorJob& J, int op) { return !J.table && J.chunks <= (op == 0 ? 32u : op == 1 ? 26u : 20u); }
+// Whether one launch does it (k_small; not where anything is in place).  Its time grows with the chunks: those of 16-bit types hold twice
+// the elements and count half more or, where an update's weights go with them, twice.  us in one / two launches, a call through Python:
+// fp32 norm of 14 chunks 5.6 / 8.8, 36 7.5 / 8.8, 44 8.6 / 8.9 (in eight tensors 9.7 / 8.8); clipped 18 6.9 / 9.3, 30 8.7 / 9.7, 36 9.6 / 9.8
+// (10.4 / 9.8); updated 30 9.1 / 9.7, 36 10.2 / 9.8; bf16 norm of 22 7.6 / 8.8, 30 9.5 / 8.9; clipped 18 9.2 / 9.8, 22 10.2 / 9.8; updated
+// 14 9.6 / 9.8, 18 10.7 / 9.9.
+bool list_is_small(const TensorJob& J, int op) {
+  constexpr unsigned MOST[3] = {80, 64, 60};   // twice the chunks of fp32
+  if (J.table || 2 * J.chunks > MOST[op]) return false;
+  unsigned cost = 2 * J.chunks;
+  for (int t = 0; t < J.tensors; ++t) {
+    const unsigned end = t + 1 < J.tensors ? J.e[t + 1].chunk : J.chunks;
+    if (J.e[t].type != ELEMENT_F32) cost += (op == 2 ? 2 : 1) * (end - J.e[t].chunk);
+  }
+  return cost <= MOST[op];
+}
 
 hipError_t launch_small(hipStream_t stream, const TensorJob& J, int op, double max_norm, double lr, float* norm) {
   const dim3 grid(op == 0 ? 1 : std::max(1u, (J.chunks + SMALL_GROUPS - 1) / SMALL_GROUPS)), threads(GT * SMALL_GROUPS);

@@ -63,6 +63,8 @@ def _check_clip(before, after, norm, limit):
 LISTS = [
     [1], [2, 0, 3], [0], [], [7], [4095, 1], [8192], [8193, 8191], [20, 320, 40, 20000, 150, 54000, 10, 1500], [1 << 20, 3, 5, 100003],
     [33] * 127, [33] * 128, [65, 1] * 65, [5] * 256 + [9000] * 2, [0] * 130 + [17], [3] * 600,
+    # entries on both sides of a lane's places and of an argument's, chunks that end in the middle of four
+    [4097] * 16, [4099] * 17, [8190] * 64, [8195] * 65, [12289, 3] * 60, [8191] * 121, [12288 + k for k in range(12)], [163840], [163841], [122881, 1],
 ]
 
 
