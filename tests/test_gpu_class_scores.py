@@ -174,6 +174,31 @@ def test_many_rows(rows, n, top, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n,top", [(1, 2, 0), (2, 16, 0), (70, 10, 3), (5, 16, 16), (9, 33, 20), (3, 64, 64), (7, 100, 20), (300, 300, 0), (4, 1000, 5),
+                                        (3, 1016, 64), (2, 65, 1), (5000, 700, 30)])
+def test_rows_that_are_nearly_sure_keep_the_digits_of_small_logarithms(rows, n, top, dtype):
+    """log p of the best class, -log(1 + R), R the sum of the others' e^-g.  A term is off by 2.5 U g (its difference, its product) and 2 U,
+    their sum by 22 U, the logarithm by 4 U and the share of R by 5 U: (2.5 g + 36) U in all."""
+    import torch
+    gen = torch.Generator(device="cuda:0").manual_seed(n)
+    gap = torch.rand(rows, n, generator=gen, device="cuda:0") * 10 + 8
+    x = (-gap).to(getattr(torch, dtype))
+    best = torch.randint(0, n, (rows,), generator=gen, device="cuda:0", dtype=torch.int32)
+    x[torch.arange(rows), best.long()] = 0.25
+    out = _call(x, best, top)
+    d = x.double().cpu().numpy()
+    g = 0.25 - d
+    for r, b in enumerate(best.tolist()):
+        d[r, b] = -np.inf
+    want = -np.log1p(np.exp(d - 0.25).sum(1))
+    tol = np.abs(want) * (2.5 * g.max() + 36) * U
+    assert (np.abs(out["lp"].cpu().numpy() - want) <= tol).all()
+    assert (np.abs(out["norm"][:, 1].cpu().numpy() + want) <= tol).all()
+    if top:
+        assert torch.equal(out["top"][:, 0], best) and torch.equal(out["top_lp"][:, 0], out["lp"])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,n,top", [(1, 9217, 64), (2, 8192, 64), (5, 65536, 20), (3, 65537, 20), (37, 50003, 25), (128, 66001, 20), (127, 66001, 20),
                                         (200, 100003, 64), (256, 30011, 8), (257, 30011, 8), (40, 102401, 0), (1, 102399, 0), (512, 8000, 5), (513, 8000, 5)])
 def test_few_long_rows(rows, n, top, dtype):
