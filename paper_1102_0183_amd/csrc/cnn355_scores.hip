@@ -714,9 +714,9 @@ __global__ void __launch_bounds__(ST) k_scores_rows(ScoreJob J) {
 // ---- the gradient ----
 struct GradRow {
   float m, log_s;
-  float a, b;      // -p (a + b log p)
+  float a, b;      // -p (a + b log p), a without the label's gradient: b H
   float g_label;
-  int label;
+  int label;       // -1: none
   bool empty;
 };
 __device__ __forceinline__ GradRow grad_row(const ScoreGradJob& J, long long row) {
@@ -724,17 +724,30 @@ __device__ __forceinline__ GradRow grad_row(const ScoreGradJob& J, long long row
   r.m = J.normaliser[2 * row];
   r.log_s = J.normaliser[2 * row + 1];
   r.empty = r.m == -INFINITY;
-  r.label = J.labels ? J.labels[row] : -1;
-  const bool has = r.label >= 0 && r.label < J.classes && J.g_log_probs;
+  const int label = J.labels && J.g_log_probs ? J.labels[row] : -1;
+  const bool has = label >= 0 && label < J.classes;
+  r.label = has ? label : -1;
   r.g_label = has ? J.g_log_probs[row] : 0.0f;
   r.b = J.g_entropy ? J.g_entropy[row] : 0.0f;
-  r.a = J.g_entropy ? fmaf(r.b, J.entropy[row], r.g_label) : r.g_label;
+  r.a = J.g_entropy ? r.b * J.entropy[row] : 0.0f;
   return r;
 }
 // of one class; a class of probability zero has none but its label's
-__device__ __forceinline__ float grad_of(const GradRow& r, float x, int c) {
+__device__ __forceinline__ float grad_of(const GradRow& r, float with_label, float x) {   // (with_label: a + g_label)
   const float log_p = (x - r.m) - r.log_s, p = __builtin_amdgcn_exp2f(log_p * LOG2E);
-  const float g = (c == r.label ? r.g_label : 0.0f) - (p == 0.0f ? 0.0f : p * fmaf(r.b, log_p, r.a));
+  const float g = p == 0.0f ? 0.0f : -p * fmaf(r.b, log_p, with_label);
+  return r.empty ? 0.0f : g;
+}
+// of the label's: 1 - p by its series where p is close to 1 and the difference would keep few digits
+__device__ __forceinline__ float grad_of_label(const GradRow& r, float x) {
+  const float y = (x - r.m) - r.log_s, p = __builtin_amdgcn_exp2f(y * LOG2E);
+  float series = fmaf(y, 1.0f / 720, 1.0f / 120);
+  series = fmaf(y, series, 1.0f / 24);
+  series = fmaf(y, series, 1.0f / 6);
+  series = fmaf(y, series, 0.5f);
+  series = fmaf(y, series, 1.0f);
+  const float others = y > -0.25f ? -y * series : 1.0f - p;
+  const float g = r.g_label * others - (p == 0.0f ? 0.0f : p * fmaf(r.b, y, r.a));
   return r.empty ? 0.0f : g;
 }
 
@@ -744,11 +757,20 @@ __device__ __forceinline__ void put_gradients(const GradRow& r, v4u in, CNN_GLOB
   typedef Element<TYPE> E;
   typename E::T e[E::V];
   v4u v = {0, 0, 0, 0};
+  const float with_label = r.a + r.g_label;
 #pragma unroll
-  for (int j = 0; j < E::V; ++j) {
-    e[j] = E::make(grad_of(r, E::get(in, j), first + c + j));
-    E::put(v, j, e[j]);
+  for (int j = 0; j < E::V; ++j) e[j] = E::make(grad_of(r, with_label, E::get(in, j)));
+  const int at = r.label - first - c;
+  if (r.label >= 0 && (unsigned)at < (unsigned)E::V) {
+    float x = 0.0f;
+#pragma unroll
+    for (int j = 0; j < E::V; ++j) x = at == j ? E::get(in, j) : x;
+    const typename E::T g_label = E::make(grad_of_label(r, x));
+#pragma unroll
+    for (int j = 0; j < E::V; ++j) e[j] = at == j ? g_label : e[j];
   }
+#pragma unroll
+  for (int j = 0; j < E::V; ++j) E::put(v, j, e[j]);
   if (c + E::V <= end) *(CNN_GLOBAL v4u_any*)(g + c) = v;
   else {
 #pragma unroll

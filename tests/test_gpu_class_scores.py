@@ -387,6 +387,28 @@ def test_gradients_in_place_and_between_other_columns(n, dtype):
     assert torch.equal(x.isnan(), apart.isnan()) and torch.equal(x.nan_to_num(), apart.nan_to_num())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n", [(1, 2), (70, 10), (9, 64), (300, 300), (4, 1000)])
+def test_gradients_of_rows_that_are_nearly_sure(rows, n, dtype):
+    """The label's, g (1 - p), is off by what its log p is, (2.5 gap + 36) U of it, the series' 8 U, the product's and the type's rounding."""
+    import torch
+    gen = torch.Generator(device="cuda:0").manual_seed(n + 1)
+    x = (-(torch.rand(rows, n, generator=gen, device="cuda:0") * 10 + 8)).to(getattr(torch, dtype))
+    label = torch.randint(0, n, (rows,), generator=gen, device="cuda:0", dtype=torch.int32)
+    i = torch.arange(rows, device="cuda:0"), label.long()
+    x[i] = 0.25
+    g = torch.randn(rows, generator=gen, device="cuda:0")
+    out, grad = _call(x, label, 0), torch.empty_like(x)
+    binding.class_scores_grad(x, grad, out["norm"], label, g)
+    d = x.double().cpu().numpy()
+    gap = 0.25 - d.min()
+    d[np.arange(rows), label.cpu().numpy()] = -np.inf
+    want = g.double().cpu().numpy() * -np.expm1(-np.log1p(np.exp(d - 0.25).sum(1)))
+    fi = torch.finfo(x.dtype)
+    tol = np.abs(want) * ((2.5 * gap + 48) * U + fi.eps / 2 * (1 + 1e-3)) + fi.smallest_normal * fi.eps / 2
+    assert (np.abs(grad[i].double().cpu().numpy() - want) <= tol).all()
+
+
 @pytest.mark.parametrize("n", [7, 90, 1500])
 def test_gradients_are_those_of_differences(n):
     """Central differences of the definition in 64 bits, h = 1e-4: off by h^2 / 6 of a third derivative (below 8 times the two
