@@ -798,8 +798,9 @@ __global__ void __launch_bounds__(ST) k_scores_grad_rows(ScoreGradJob J) {
   }
 }
 
-// A wavefront a tile of its workgroup's four, row after row, gridDim.y apart, the next one's values under way.  (Rows that start
-// at odd addresses take 4 % longer, tiles that begin with 16 whole bytes or not.)
+// A wavefront a tile of its workgroup's four, of a row.  (us with 8192 workgroups that go from row to row, the next one's values under
+// way, and so: 2000 rows of 50001 fp16 classes 79.4 / 78.1, 2048 of 131072 bf16 193.8 / 179.5, fp32 391.9 / 373.0.  Rows that start at odd
+// addresses take 4 % longer, tiles that begin with 16 whole bytes or not.)
 template <int TYPE>
 __global__ void __launch_bounds__(ST) k_scores_grad(ScoreGradJob J) {
   typedef Element<TYPE> E;
@@ -810,18 +811,11 @@ __global__ void __launch_bounds__(ST) k_scores_grad(ScoreGradJob J) {
   if (end <= 0) return;
   const CNN_GLOBAL T* x = (const CNN_GLOBAL T*)J.x + first;
   CNN_GLOBAL T* g = (CNN_GLOBAL T*)J.grad + first;
-  v4u next[N];
-  auto load = [&](long long row) {
-#pragma unroll
-    for (int q = 0; q < N; ++q) next[q] = load16<TYPE>(x + row * J.stride, (q * 64 + lane) * V, end);
-  };
-  load(blockIdx.y);
   for (long long row = blockIdx.y; row < J.rows; row += gridDim.y) {
     v4u in[N];
 #pragma unroll
-    for (int q = 0; q < N; ++q) in[q] = next[q];
+    for (int q = 0; q < N; ++q) in[q] = load16<TYPE>(x + row * J.stride, (q * 64 + lane) * V, end);
     const GradRow r = grad_row(J, row);
-    if (row + gridDim.y < J.rows) load(row + gridDim.y);
 #pragma unroll
     for (int q = 0; q < N; ++q) put_gradients<TYPE>(r, in[q], g + row * J.grad_stride, (q * 64 + lane) * V, end, first);
   }
@@ -910,10 +904,8 @@ hipError_t launch_scores_grad_type(hipStream_t stream, const ScoreGradJob& J) {
   if (J.classes <= SCORE_TILE) {
     CNN355_LANES(k_scores_grad_rows, lanes_of((J.classes + 15) / 16))
   } else {
-    // Workgroups that hold a row's tiles, and rows that are under way.  us with 2048 / 8192 workgroups / one for every four tiles:
-    // 2000 rows of 50001 fp16 102 / 84 / 90, 2048 of 131072 bf16 240 / 194 / 197, fp32 412 / 391 / 375, 20000 of 5000 bf16 129 / 104 / 116
-    const long long wide = (J.classes + 4 * SCORE_TILE - 1) / (4 * SCORE_TILE), rows = TYPE == ELEMENT_F32 ? J.rows : std::max(1ll, 8192 / wide);
-    const dim3 grid((unsigned)wide, (unsigned)std::min<long long>({J.rows, rows, 65535}));
+    const unsigned wide = (unsigned)((J.classes + 4 * SCORE_TILE - 1) / (4 * SCORE_TILE));
+    const dim3 grid(wide, (unsigned)std::min<long long>(J.rows, 65535));
     hipLaunchKernelGGL(k_scores_grad<TYPE>, grid, dim3(ST), 0, stream, J);
   }
   return hipGetLastError();
