@@ -798,26 +798,27 @@ __global__ void __launch_bounds__(ST) k_scores_grad_rows(ScoreGradJob J) {
   }
 }
 
-// A wavefront a tile of its workgroup's four, of a row.  (us with 8192 workgroups that go from row to row, the next one's values under
-// way, and so: 2000 rows of 50001 fp16 classes 79.4 / 78.1, 2048 of 131072 bf16 193.8 / 179.5, fp32 391.9 / 373.0.  Rows that start at odd
+// A wavefront a tile, row after row.  us with 8192 workgroups that go from row to row, the next one's values under way, / a workgroup
+// for four tiles of one row / so: 2000 rows of 50001 fp16 classes 79.4 / 78.1 / 77.9, 2048 of 131072 bf16 193.8 / 180 / 187, of fp32 392 /
+// 373 / 373, 20000 of 5000 bf16 101 / 104 / 79, of fp32 186 / 176 / 144, 150000 of 1500 bf16 - / 258 / 192.  (Rows that start at odd
 // addresses take 4 % longer, tiles that begin with 16 whole bytes or not.)
 template <int TYPE>
-__global__ void __launch_bounds__(ST) k_scores_grad(ScoreGradJob J) {
+__global__ void __launch_bounds__(ST) k_scores_grad(ScoreGradJob J, unsigned tiles, unsigned units) {
   typedef Element<TYPE> E;
   typedef typename E::T T;
   constexpr int V = E::V, N = 16 / V;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int first = (blockIdx.x * (ST / 64) + wave) * SCORE_TILE, end = J.classes - first;
-  if (end <= 0) return;
-  const CNN_GLOBAL T* x = (const CNN_GLOBAL T*)J.x + first;
-  CNN_GLOBAL T* g = (CNN_GLOBAL T*)J.grad + first;
-  for (long long row = blockIdx.y; row < J.rows; row += gridDim.y) {
+  const int lane = threadIdx.x & 63;
+  for (unsigned unit = blockIdx.x * (ST / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); unit < units; unit += gridDim.x * (ST / 64)) {
+    const long long row = unit / tiles;
+    const int first = (int)(unit % tiles) * SCORE_TILE, end = J.classes - first;
+    const CNN_GLOBAL T* x = (const CNN_GLOBAL T*)J.x + row * J.stride + first;
+    CNN_GLOBAL T* g = (CNN_GLOBAL T*)J.grad + row * J.grad_stride + first;
     v4u in[N];
 #pragma unroll
-    for (int q = 0; q < N; ++q) in[q] = load16<TYPE>(x + row * J.stride, (q * 64 + lane) * V, end);
+    for (int q = 0; q < N; ++q) in[q] = load16<TYPE>(x, (q * 64 + lane) * V, end);
     const GradRow r = grad_row(J, row);
 #pragma unroll
-    for (int q = 0; q < N; ++q) put_gradients<TYPE>(r, in[q], g + row * J.grad_stride, (q * 64 + lane) * V, end, first);
+    for (int q = 0; q < N; ++q) put_gradients<TYPE>(r, in[q], g, (q * 64 + lane) * V, end, first);
   }
 }
 
@@ -904,9 +905,9 @@ hipError_t launch_scores_grad_type(hipStream_t stream, const ScoreGradJob& J) {
   if (J.classes <= SCORE_TILE) {
     CNN355_LANES(k_scores_grad_rows, lanes_of((J.classes + 15) / 16))
   } else {
-    const unsigned wide = (unsigned)((J.classes + 4 * SCORE_TILE - 1) / (4 * SCORE_TILE));
-    const dim3 grid(wide, (unsigned)std::min<long long>(J.rows, 65535));
-    hipLaunchKernelGGL(k_scores_grad<TYPE>, grid, dim3(ST), 0, stream, J);
+    const long long tiles = (J.classes + SCORE_TILE - 1) / SCORE_TILE, units = J.rows * tiles;
+    if (units > 1ll << 31) return hipErrorInvalidValue;   // (no memory holds so many)
+    hipLaunchKernelGGL(k_scores_grad<TYPE>, dim3(grid_of(units, ST / 64)), dim3(ST), 0, stream, J, (unsigned)tiles, (unsigned)units);
   }
   return hipGetLastError();
 }

@@ -387,6 +387,26 @@ def test_gradients_in_place_and_between_other_columns(n, dtype):
     assert torch.equal(x.isnan(), apart.isnan()) and torch.equal(x.nan_to_num(), apart.nan_to_num())
 
 
+def test_gradients_of_more_rows_than_a_launch_holds():
+    """In place, on a buffer whose places pass 32 bits; a row's gradient is its own, whatever the number of rows."""
+    import torch
+    rows, n = (1 << 21) + 3, 1025
+    some, l = _rows(4097, n, "bfloat16", 8)
+    x = some.repeat(-(-rows // 4097), 1)[:rows]
+    labels = l.repeat(-(-rows // 4097))[:rows].contiguous()
+    out = _call(some, l, 0)
+    norm, h = (out[k].repeat(*([-(-rows // 4097)] + [1] * (out[k].dim() - 1)))[:rows].contiguous() for k in ("norm", "h"))
+    gen = torch.Generator(device="cuda:0").manual_seed(3)
+    g, e = (torch.randn(rows, generator=gen, device="cuda:0") for _ in range(2))
+    binding.class_scores_grad(x, x, norm, labels, g, h, e)
+    for a in (0, 4097, 1 << 20, rows - 4097 - rows % 4097, rows - rows % 4097):
+        a -= a % 4097
+        b = min(rows, a + 4097)
+        want = torch.empty_like(some[:b - a])
+        binding.class_scores_grad(some[:b - a], want, norm[a:b], l[:b - a], g[a:b], h[a:b], e[a:b])
+        assert torch.equal(x[a:b], want), a
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,n", [(1, 2), (70, 10), (9, 64), (300, 300), (4, 1000)])
 def test_gradients_of_rows_that_are_nearly_sure(rows, n, dtype):
