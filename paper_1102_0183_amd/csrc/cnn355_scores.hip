@@ -413,10 +413,13 @@ __device__ __forceinline__ void load_tile(v4u (&r)[16 / Element<TYPE>::V], const
 //
 // In the usual tile the exponent is one operation, d = x / ln 2 - r, with a lane's r as m / ln 2 was when it was last above r by
 // more than GROWTH (then both sums go to the new r): every e is too large by the same 2^(m / ln 2 - r), which is taken out at
-// the end.  A masked class gives 0 (-inf) there, and values near the type's lowest and highest leave the range of d; a tile that
-// has any shows it in its sums, is done again with d = (x - m) / ln 2 and the product of e and d clamped, and so are those behind
-// it (two operations more for each class).
+// the end.  Not every tile is usual.  A masked class gives 0 (-inf) there, and values near the type's lowest leave the range of d,
+// which shows in the sums.  And r is rounded while x / ln 2 is not: from 2^24 on d is off by more than a half for the largest class
+// itself, and soon so far that every e is 0 (or all are infinite); so a lane whose r would be no smaller than that makes its sum
+// one that shows (FUSED: 11.6 million as a value, more than fp16 holds).  Such a tile is done again with d = (x - m) / ln 2 and the
+// product of e and d clamped, and so are those behind it (two operations more for each class).
 constexpr float GROWTH = 8.0f;   // (t is off by r's distance from m times the rounding of s)
+constexpr float FUSED = 16777216.0f;
 template <int TYPE, bool ENTROPY, bool TOP>
 __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step, int last, int n_top, Sums& a, Best& b, Picking* L) {
 #pragma clang fp contract(off)   // (r is the rounded product in the difference of two of them, too)
@@ -457,7 +460,7 @@ __device__ __forceinline__ void scan(const RowAt<TYPE>& row, int first, int step
         to = grown ? m * LOG2E : r;
         const float d0 = r - to, f = __builtin_amdgcn_exp2f(d0);
         t = fmaf(fmaxf(d0, FAR), s, t) * f;
-        s *= f;
+        s = fabsf(to) < FUSED ? s * f : __builtin_nanf("");
       }
 #pragma unroll
       for (int k = 0; k < 16; ++k) {

@@ -469,3 +469,44 @@ def test_bad_tensors_are_refused():
             binding.class_scores(x, **kw)
     with pytest.raises(binding.CnnError):
         binding.class_scores(x, d_log_probs=f)
+
+
+FAR = [1.1e7, 1.2e7, 2e7, 1e8, 1e9, 5e9, 1e10, 1e12, 1e15, 1e20, 1e30, 1e36, 1.5e38, 2.3e38, 3.3e38]
+
+
+def _far_rows(n, dtype, values):
+    """Rows of values v, for v of both signs far from 0: constant, as far as v from each other, rising to v and falling from it, half of
+    them masked, and one class at v among ordinary ones, the first, in the middle, the last."""
+    import torch
+    gen = torch.Generator(device="cuda:0").manual_seed(n)
+    rand = lambda: torch.randn(n, generator=gen, device="cuda:0")  # noqa: E731
+    rise = torch.arange(1, n + 1, device="cuda:0") / n
+    rows = []
+    for v in values:
+        for s in (v, -v):
+            masked = torch.full((n,), s, device="cuda:0")
+            masked[::2] = -math.inf
+            rows += [torch.full((n,), s, device="cuda:0"), rand().clamp(-3, 3) / 3 * s, rise * s, rise.flip(0) * s, masked]
+        for at in (0, n // 2, n - 1):
+            rows.append(rand())
+            rows[-1][at] = v
+    return torch.stack(rows).to(getattr(torch, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,top", [(40, 20), (200, 20), (900, 5), (1024, 20), (3000, 20), (9001, 3), (30000, 64), (70001, 20), (110000, 2)])
+def test_finite_values_far_from_zero(n, top, dtype):
+    """Every finite row has a distribution, whatever its size: with all outputs, without the entropy, without the best, and the
+    gradient from those normalisers.  (The longest in parts of rows.)"""
+    import torch
+    x = _far_rows(n, dtype, FAR if n <= 5000 else FAR[n % 4::4])
+    rows = x.shape[0]
+    labels = (torch.arange(rows, device="cuda:0", dtype=torch.int32) * 7919) % n
+    every = _call(x, labels, top)
+    assert torch.isfinite(every["norm"]).all() and (every["top"] >= 0).all()
+    _check(x, labels, top, every)
+    for want in (("lp", "norm"), ("lp", "top", "top_lp")):
+        out = _call(x, labels, top, want=want)
+        _check(x, labels, top, {**every, **{k: out[k] for k in want}})
+    g = torch.randn(2, rows, generator=torch.Generator(device="cuda:0").manual_seed(2), device="cuda:0")
+    _check_grad(x, labels, g[0].contiguous(), g[1].contiguous())
