@@ -564,13 +564,17 @@ __global__ void __launch_bounds__(threads_of(WAVES)) k_scores(ScoreJob J) {
     }
     if (TOP) b.list = with_masked<TYPE>(J, row, b.list);
     float rest = a.s - 1.0f;
-    if (WAVES == 1 && x.end <= SCORE_TILE && __ballot(a.s < SURE)) {   // (its tile from the cache)
+    if (WAVES == 1 && J.classes <= SCORE_TILE && __ballot(a.s < SURE)) {   // (from the cache; from its first class on, wherever that lies:
+      typedef typename Element<TYPE>::T T;                                 // a lane has the same classes of equal rows, 16 at most)
       constexpr int V = Element<TYPE>::V;
-      v4u r[16 / V];
-      load_tile<TYPE>(r, x, 0);
+      const CNN_GLOBAL T* from = (const CNN_GLOBAL T*)J.x + row * J.stride;
       float v[16];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = Element<TYPE>::get(r[k / V], k % V);
+      for (int q = 0; q < 16 / V; ++q) {
+        const v4u r = load16<TYPE>(from, (q * 64 + lane) * V, J.classes);
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[q * V + k] = Element<TYPE>::get(r, k);
+      }
       rest = rest_of<64>(a, v);
     }
     give_row(J, row, lane, a, rest, label, b.list);

@@ -510,3 +510,30 @@ def test_finite_values_far_from_zero(n, top, dtype):
         _check(x, labels, top, {**every, **{k: out[k] for k in want}})
     g = torch.randn(2, rows, generator=torch.Generator(device="cuda:0").manual_seed(2), device="cuda:0")
     _check_grad(x, labels, g[0].contiguous(), g[1].contiguous())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pad,offset", [(0, 1), (1, 0), (3, 5), (5, 7)])
+@pytest.mark.parametrize("n,top", [(1017, 9), (1018, 64), (1019, 20), (1022, 9), (1023, 33), (1024, 64), (1024, 9)])
+def test_nearly_sure_rows_are_the_same_wherever_they_start(n, top, pad, offset, dtype):
+    """Rows of equal values, at every distance from a 16-byte boundary: the same logarithms to the last bit, and those of the definition
+    to the (2.5 g + 36) U of the test of aligned ones above."""
+    import torch
+    rows = 16
+    gen = torch.Generator(device="cuda:0").manual_seed(n)
+    one = (-(torch.rand(n, generator=gen, device="cuda:0") * 10 + 13)).to(getattr(torch, dtype))
+    one[n // 3] = 0.25
+    wide = torch.zeros(rows * (n + pad) + offset, dtype=one.dtype, device="cuda:0")
+    x = wide[offset:].view(rows, n + pad)[:, :n]
+    x.copy_(one.expand(rows, n))
+    labels = torch.full((rows,), n // 3, dtype=torch.int32, device="cuda:0")
+    out = _call(x, labels, top)
+    d = one.double().cpu().numpy()
+    gap = 0.25 - d.min()
+    d[n // 3] = -np.inf
+    want = -np.log1p(np.exp(d - 0.25).sum())
+    tol = abs(want) * (2.5 * gap + 36) * U
+    assert (np.abs(out["lp"].cpu().numpy().astype(np.float64) - want) <= tol).all()
+    assert (np.abs(out["norm"][:, 1].cpu().numpy().astype(np.float64) + want) <= tol).all()
+    for k in ("lp", "norm", "top", "top_lp"):
+        assert torch.equal(out[k], out[k][:1].expand_as(out[k])), k
