@@ -537,3 +537,29 @@ def test_nearly_sure_rows_are_the_same_wherever_they_start(n, top, pad, offset, 
     assert (np.abs(out["norm"][:, 1].cpu().numpy().astype(np.float64) + want) <= tol).all()
     for k in ("lp", "norm", "top", "top_lp"):
         assert torch.equal(out[k], out[k][:1].expand_as(out[k])), k
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n,top", [(300, 8, 3), (300, 700, 20), (300, 1500, 9), (300, 1500, 0), (300, 9000, 5), (64, 30000, 5), (40, 90000, 20), (40, 110000, 0)])
+def test_no_probability_is_above_one(rows, n, top, dtype):
+    """Rows with a class beside which the others are nothing: its log p, above -n e^-39, is 0 to the tolerance of the definition (rows of up
+    to 1024 classes: to that number), and not above it."""
+    import torch
+    gen = torch.Generator(device="cuda:0").manual_seed(n)
+    best = torch.randint(0, n, (rows,), generator=gen, device="cuda:0", dtype=torch.int32)
+    m = torch.rand(rows, generator=gen, device="cuda:0") * 40 - 20
+    m[1::4] *= 1500
+    m = m.to(getattr(torch, dtype)).double()
+    x = (m - 40 - m.abs() / 8)[:, None].expand(rows, n).contiguous()
+    i = torch.arange(rows, device="cuda:0"), best.long()
+    x[i] = m
+    x = x.to(getattr(torch, dtype))
+    out = _call(x, best, top)
+    off = n * 2e-17 + (0 if n <= 1024 else (_terms(rows, n) + 100) * U)
+    assert (out["lp"] <= 0).all() and (out["lp"] >= -off).all()
+    assert (out["norm"][:, 1] >= 0).all() and (out["norm"][:, 1] <= off).all() and (out["h"] >= 0).all()
+    if top:
+        assert torch.equal(out["top"][:, 0], best) and (out["top_lp"] <= 0).all()
+    grad = torch.empty_like(x)
+    binding.class_scores_grad(x, grad, out["norm"], best, torch.ones(rows, device="cuda:0"))
+    assert (grad[i] >= 0).all()
