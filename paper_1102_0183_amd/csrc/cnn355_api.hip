@@ -2942,7 +2942,8 @@ int cnn355_deform_form(int C, int H, int W, float sigma) {
 
 // tap_step >= 0 (parity tap): the pass stops behind that trainable layer and its outputs for the n <= batch
 // images, [image][out_per_image], are copied to host_tap; d_probs is not written then.  scores: the pass ends with the output
-// layer's sums, and what is asked for of them (d_probs is not written either).
+// layer's sums, and what is asked for of them (d_probs is not written either).  A sum that is no number stays one there, whichever
+// kernel adds it up; the output units' passes count it as -inf where it comes in planes.
 static int forward_batch_impl(cnn_t* net, const float* d_images, size_t n, float* d_probs, void* d_scratch,
                               size_t scratch_bytes, size_t batch, int tap_step, float* host_tap, size_t* tap_per_image,
                               const ScoreJob* scores = nullptr) {
@@ -3041,6 +3042,7 @@ static int forward_batch_impl(cnn_t* net, const float* d_images, size_t n, float
       if (raw && !add) {
         BatchPool q = st.pool;
         q.sums = d_sums; q.out = out; q.total = (long long)nb * q.Mo * q.Hp * q.Wp;
+        if (scores && s + 1 == B.steps.size()) q.act = OUT_SUMS;
         HIP_TRY(net, launch_batch_pool(net->stream, q));
       }
       if (tail) {
@@ -3049,7 +3051,7 @@ static int forward_batch_impl(cnn_t* net, const float* d_images, size_t n, float
         BatchTail t;
         t.in = add ? d_sums : out; t.bias_h = add ? st.pool.bias : nullptr; t.w = L.w; t.bias = L.bias; t.out = probs;
         t.n = (long long)nb; t.slice_stride = st.pool.slice_stride; t.n_slices = add ? st.pool.n_slices : 1;
-        t.n_hidden = L.n_in; t.n_out = L.n_out; t.out_units = units; t.drop = B.steps.back().raw();
+        t.n_hidden = L.n_in; t.n_out = L.n_out; t.out_units = units; t.drop = !scores && B.steps.back().raw();
         HIP_TRY(net, launch_batch_tail(net->stream, t));
         done = true;
         break;

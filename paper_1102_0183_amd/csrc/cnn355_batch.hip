@@ -1438,7 +1438,8 @@ __device__ __forceinline__ float add_planes(cgf p, int n, long long stride) {
 // bias + scaled tanh + max-pooling (Sec. 2.2, 2.3) of the raw sums of a whole batch; the sums may
 // come as several planes (slices of the k range), added here in a fixed order.  The activation
 // function is increasing, so the maximum is taken first: one tanh per window.  act 0: none (the
-// output layer's sums go on to the output units).
+// output layer's sums go on to the output units).  A window's sum that is no number does not count;
+// act OUT_SUMS (the output layer's, windows of one): none, and such a sum stays one.
 __global__ void __launch_bounds__(256) k_batch_pool(BatchPool q) {
   const long long x = (long long)blockIdx.x * 256 + threadIdx.x;
   if (x >= q.total) return;
@@ -1452,10 +1453,10 @@ __global__ void __launch_bounds__(256) k_batch_pool(BatchPool q) {
   for (int dy = 0; dy < q.Kp; ++dy)
     for (int dx = 0; dx < q.Kpx; ++dx) {
       const float v = add_planes(src + dy * q.Wo + dx, q.n_slices, q.slice_stride);
-      best = fmaxf(best, v);
+      best = q.act == OUT_SUMS ? v : fmaxf(best, v);
     }
   best += q.bias[j];
-  q.out[x] = q.act ? b_act(best) : best;
+  q.out[x] = q.act == 1 ? b_act(best) : best;
 }
 
 // Output units of a whole batch: soft-max of the output layer's sums (as n_slices planes without the bias, or one with
@@ -1469,10 +1470,11 @@ __global__ void __launch_bounds__(256) k_batch_outputs(cgf sums, int n_slices, l
   cgf v = a;
   if (bias || out_units == 1) {
     for (int k = 0; k < n_classes; ++k) {
-      const float x = bias ? fmaxf(add_planes(a + k, n_slices, slice_stride), -INFINITY) + bias[k] : a[k];
+      float x = bias ? add_planes(a + k, n_slices, slice_stride) : a[k];
+      if (bias) x = (out_units == OUT_SUMS ? x : fmaxf(x, -INFINITY)) + bias[k];
       o[k] = out_units == 1 ? b_act(x) : x;
     }
-    if (out_units != 0) return;   // (OUT_SUMS: the sums as they are)
+    if (out_units != 0) return;   // (OUT_SUMS: the sums as they are, no numbers too)
     v = o;
   }
   // (sums that are there already are read where they are: through the outputs, 1000 classes took 1.25 times as long)

@@ -380,7 +380,7 @@ struct BatchPool {
   long long total;               // batch * Mo * Hp * Wp
   long long slice_stride;        // floats between the planes of partial sums
   int Mo, Ho, Wo, Kp, Kpx, Hp, Wp, n_slices;  // pooling window Kp rows x Kpx columns
-  int act;                       // 1: scaled tanh, 0: none
+  int act;                       // 1: scaled tanh, 0: none, OUT_SUMS: none, and sums that are no number stay so
 };
 struct BatchPack {
   const CNN_GLOBAL float* w;     // conv: [n_conn][K*Kx] in table order; fc: [n_out][n_in]

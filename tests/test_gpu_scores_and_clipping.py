@@ -7,7 +7,7 @@ import pytest
 
 import oracle
 from paper_1102_0183_amd import binding, synth
-from tests.parity_helpers import TOL_ACT, build_pair, to_dev
+from tests.parity_helpers import TOL_ACT, build_pair, layer_bounds, to_dev
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -294,3 +294,40 @@ def test_an_output_layer_trained_with_all_of_them(rows, width, classes, captured
         off += scale * (e + float(gw.abs().max()) * share) + U * float(w64.abs().max())
         w64, b64 = w64 - scale * gw, b64 - scale * gb
         assert (w.double().cpu() - w64).abs().max() <= off and (b.double().cpu() - b64).abs().max() <= off
+
+
+@pytest.mark.parametrize("name,arch", NETS)
+@pytest.mark.parametrize("n,batch", [(1, 1), (7, 7), (50, 16), (300, 300)])
+def test_a_sum_that_is_no_number(name, arch, n, batch):
+    """A weight of NaN in the output layer: its class's sum is NaN for every image, whichever kernels add it up, so that no image has
+    a distribution; and as before once the weight is a number again."""
+    import torch
+    g, o, images = _pair(name, arch)
+    C, top = g.num_classes, min(g.num_classes, 3)
+    d_imgs = to_dev(images(n))
+    labels = torch.arange(n, dtype=torch.int32, device="cuda:0") % C
+    labels[n // 2] = C
+    scratch = torch.empty(g.forward_batch_scratch_bytes(batch), dtype=torch.uint8, device="cuda:0")
+
+    def scores():
+        lp, h, best = (torch.full(s, 9.0, device="cuda:0") for s in ((n,), (n,), (n, top)))
+        which = torch.full((n, top), 9, dtype=torch.int32, device="cuda:0")
+        torch.cuda.synchronize()
+        g.score_batch(d_imgs, n, scratch, batch, labels, lp, h, which, best)
+        g.synchronize()
+        return lp, h, which, best
+
+    weights = g.get_weights()
+    first = scores()
+    begin, end = layer_bounds(o)[-1]
+    inputs = (end - begin) // C - 1
+    for k in (0, C - 1):
+        bad = weights.copy()
+        bad[begin + C + k * inputs + inputs // 2] = math.nan
+        g.set_weights(bad)
+        lp, h, which, best = scores()
+        has = labels < C
+        assert lp[has].isnan().all() and (lp[~has] == 0).all() and h.isnan().all() and (which == -1).all() and best.isnan().all()
+    g.set_weights(weights)
+    assert all(torch.equal(a, b) for a, b in zip(first, scores()))
+    g.close()
