@@ -225,10 +225,10 @@ int cnn_train_step(cnn_t* net, const float* d_image, int32_t label, float lr);
 int cnn_train_many(cnn_t* net, const float* d_images, const int32_t* d_labels, size_t n, float lr);
 
 /* n train steps whose gradients are clipped: w <- w - lr f dE/dw, f = max_norm / N where the 2-norm N of all of an image's
- * gradients is above max_norm, else 1 (cnn_clipped_update, below, on the network's own gradients and weights; a norm that is
- * infinite or NaN leaves the weights as they are).  d_norms: [n] receives N of every image (0 where it was skipped for its
- * label), or NULL.  Every image's gradients go through memory, so the weights cannot stay on the chip between images: two
- * launches an image more than cnn_train_step.  max_norm >= 0, lr finite (CNN_E_ARG).  Asynchronous. */
+ * gradients is above max_norm, else 1 (cnn_clipped_update, below, on the network's own gradients and weights; gradients that
+ * hold an infinity or NaN leave the weights as they are).  d_norms: [n] receives N of every image, rounded as there (0 where it
+ * was skipped for its label), or NULL.  Every image's gradients go through memory, so the weights cannot stay on the chip
+ * between images: two launches an image more than cnn_train_step.  max_norm >= 0, lr finite (CNN_E_ARG).  Asynchronous. */
 int cnn_train_many_clipped(cnn_t* net, const float* d_images, const int32_t* d_labels, size_t n, float lr,
                            float max_norm, float* d_norms);
 
@@ -455,9 +455,10 @@ int cnn_class_scores_grad(void* hip_stream, const void* d_logits, int type, size
  *   cnn_clip_gradients: out = f g, of the gradients' types, rounded to fp32 and from there to them.  host_out == NULL:
  *                       in place (not written at all where f is 1)
  *   cnn_clipped_update: w <- w - lr f g for fp32 weights and gradients of any type (Sec. 3.4's adjustment)
- * A norm that is infinite or NaN changes nothing: out = g, weights stay, and *d_norm (NULL where it is not wanted,
- * but in cnn_gradient_norm) tells.  Squares, their sum, f and the update's product are double; the result depends on
- * the list alone, bit for bit.
+ * Squares, their sum, N, f and the update's product are double, so N is finite for all finite gradients; one that is
+ * infinite or NaN makes N so, and then nothing changes: out = g, weights stay.  *d_norm (NULL where it is not wanted, but
+ * in cnn_gradient_norm) is N rounded to fp32: infinite or NaN in that case, and infinite too where finite gradients have an
+ * N above 3.4e38, which are clipped and used as any others.  The result depends on the list alone, bit for bit.
  * host_grads, host_out, host_weights: host arrays of n tensors (read before the call returns) of device memory,
  * elements contiguous, sizes and types (weights: CNN_TYPE_F32) of the same order; a size may be 0.  At most 2^24
  * tensors, of 2^43 elements together.  What is written must overlap nothing else in the call, but out[i] may be

@@ -227,3 +227,28 @@ def test_streams_and_a_captured_step():
         binding.clipped_update(wl, gl, 0.01, 0.5, scratch, d_norm=norm)
         torch.cuda.synchronize()
         assert torch.equal(w, replayed) and torch.equal(norm, n) and not torch.equal(w, keep)
+
+
+@pytest.mark.parametrize("count", [1000, 300000])
+def test_a_norm_above_the_range_of_floats(count):
+    """Finite gradients have a finite norm in double, which decides: they are clipped, and weights updated, where the fp32 that is given
+    out is infinite.  (One launch and two.)"""
+    import torch
+    big = torch.full((count,), 3e38, device="cuda:0")
+    big[::3] = -2.5e38
+    before, norm = big.clone(), _norm([big])
+    n = torch.zeros(1, device="cuda:0")
+    out = [torch.empty_like(big)]
+    binding.clip_gradients(binding.TensorList([big]), 2.0, _scratch(1), out=binding.TensorList(out), d_norm=n)
+    assert math.isinf(float(n))
+    _check_clip([before], out, norm, 2.0)
+    w = torch.linspace(-1, 1, count, device="cuda:0")
+    w0 = w.double()
+    n.zero_()
+    binding.clipped_update(binding.TensorList([w]), binding.TensorList([big]), 0.5, 2.0, _scratch(1), d_norm=n)
+    assert math.isinf(float(n)) and torch.equal(big, before)
+    step = 0.5 * 2.0 / norm
+    want = w0 - step * before.double()
+    assert ((w.double() - want).abs() <= want.abs() * U + step * before.double().abs() * U * 1e-3).all()
+    binding.clip_gradients(binding.TensorList([big]), 2.0, _scratch(1), d_norm=n)
+    assert math.isinf(float(n)) and torch.equal(big, out[0])
