@@ -228,7 +228,8 @@ int cnn_train_many(cnn_t* net, const float* d_images, const int32_t* d_labels, s
  * gradients is above max_norm, else 1 (cnn_clipped_update, below, on the network's own gradients and weights; gradients that
  * hold an infinity or NaN leave the weights as they are).  d_norms: [n] receives N of every image, rounded as there (0 where it
  * was skipped for its label), or NULL.  Every image's gradients go through memory, so the weights cannot stay on the chip
- * between images: two launches an image more than cnn_train_step.  max_norm >= 0, lr finite (CNN_E_ARG).  Asynchronous. */
+ * between images: one launch an image more than cnn_train_step up to 122880 weights, two from there on.  max_norm >= 0, lr
+ * finite (CNN_E_ARG).  Asynchronous. */
 int cnn_train_many_clipped(cnn_t* net, const float* d_images, const int32_t* d_labels, size_t n, float lr,
                            float max_norm, float* d_norms);
 
