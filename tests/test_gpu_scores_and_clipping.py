@@ -331,3 +331,62 @@ def test_a_sum_that_is_no_number(name, arch, n, batch):
     g.set_weights(weights)
     assert all(torch.equal(a, b) for a, b in zip(first, scores()))
     g.close()
+
+
+WIDE = [("cfg5", mode) for mode in MODES] + [("cfg4a", binding.MODE_STAGES), ("cfg4a", binding.MODE_RESIDENT), ("cfg4b", binding.MODE_STAGES)]
+
+
+@pytest.mark.parametrize("name,mode", WIDE)
+def test_an_image_with_a_bad_label_is_passed_over_by_a_large_net(name, mode):
+    """As above where the update is two launches: the first has added up what gradients were left, the second leaves all alone."""
+    import torch
+    wl = synth.WORKLOADS[name]
+    imgs, labs = synth.images(wl, 4), synth.labels(wl, 4)
+    d_imgs = to_dev(imgs)
+    weights, norms = [], []
+    for bad in (True, False):
+        g, _ = build_pair(wl)
+        assert g.num_weights > 30 * 4096
+        g.set_mode(mode)
+        d_labs = to_dev(np.array([labs[0], -3, wl.n_classes, labs[3]], dtype=np.int32)) if bad else to_dev(labs[[0, 3]].copy())
+        norms.append(torch.full((4,), -1.0, device="cuda:0"))
+        g.train_many_clipped(d_imgs if bad else d_imgs[[0, 3]].contiguous(), d_labs, 0.05, 0.2, norms[-1] if bad else norms[-1][:2])
+        if bad:
+            with pytest.raises(binding.CnnError) as e:
+                g.synchronize()
+            assert e.value.code == binding.E_ARG
+        g.synchronize()
+        weights.append(g.get_weights())
+        g.close()
+    np.testing.assert_array_equal(*weights)
+    assert (norms[0][1:3] == 0).all() and torch.equal(norms[0][[0, 3]], norms[1][:2]) and (norms[1][:2] > 0).all()
+
+
+@pytest.mark.parametrize("name,mode", WIDE)
+def test_clipped_steps_of_a_large_net(name, mode):
+    """As test_clipped_steps, limits on both sides of the norms, with the winners' and the matrix cores' stages: every step clips, or none."""
+    import torch
+    wl = synth.WORKLOADS[name]
+    g, _ = build_pair(wl)
+    r, _ = build_pair(wl)
+    for net in (g, r):
+        net.set_mode(mode)
+    n, lr = 3, 0.05
+    imgs, labs = synth.images(wl, n), synth.labels(wl, n)
+    d_imgs, d_labs = to_dev(imgs), to_dev(labs)
+    norm = torch.full((1,), -1.0, device="cuda:0")
+    for t in range(n):
+        for share in (0.37, 1.7):
+            before = g.get_weights().astype(np.float64)
+            r.set_weights(before.astype(np.float32))
+            grad = r.debug_gradients(d_imgs[t].contiguous(), int(labs[t])).astype(np.float64)
+            N = math.sqrt(math.fsum(grad * grad))
+            limit = float(np.float32(share * N))
+            g.train_many_clipped(d_imgs[t:], d_labs[t:], lr, limit, norm, n=1)
+            g.synchronize()
+            assert abs(float(norm) - N) <= N * U * (1 + 1e-6)
+            step = float(np.float32(lr)) * (limit / N if share < 1 else 1.0)
+            want = before - step * grad
+            assert (np.abs(g.get_weights() - want) <= np.abs(want) * U + step * np.abs(grad) * U * 1e-3).all()
+    for net in (g, r):
+        net.close()
