@@ -174,6 +174,9 @@ __device__ __forceinline__ void join_lanes(Sums& a) {
 // digits.  Rows of up to 1024 classes whose sum is below SURE are summed again, a lane's 16 places x, the largest value's classes apart
 // (for all rows, 100000 of 1000 bf16 classes took 84 us, so 67; longer rows have more others).  The result: s - 1.
 constexpr float SURE = 1.5f;
+// the rest of a row that `scan` has summed: the largest value's own term is a product of two powers of two there, which may round to
+// less than 1 (in row_of, where the other kernels' rows have it too, 100000 rows of 1000 bf16 classes took 1 % longer)
+__device__ __forceinline__ float rest_of(const Sums& a) { return a.s == 0.0f ? -1.0f : fmaxf(a.s - 1.0f, 0.0f); }
 template <int LANES, int N>
 __device__ __forceinline__ float rest_of(const Sums& a, const float (&x)[N]) {
   float rest = a.s - 1.0f;
@@ -206,8 +209,6 @@ __device__ __forceinline__ Row row_of(const Sums& a, float rest) {
   if (r.none) { r.m = r.log_s = r.entropy = __builtin_nanf(""); return r; }
   const bool empty = a.s == 0.0f;
   r.m = empty ? -INFINITY : a.m;
-  // (the largest value's own term is a product of two powers of two in `scan`, which may round to less than 1)
-  rest = empty ? rest : fmaxf(rest, 0.0f);
   // log(1 + rest): of u, and where that is small by the share of rest in u - 1 (log1pf: 20000 rows of 64 classes 17.5 us, so 15.1)
   const float u = 1.0f + rest;
   r.log_s = logf(u);
@@ -565,7 +566,7 @@ __global__ void __launch_bounds__(threads_of(WAVES)) k_scores(ScoreJob J) {
       continue;
     }
     if (TOP) b.list = with_masked<TYPE>(J, row, b.list);
-    float rest = a.s - 1.0f;
+    float rest = rest_of(a);
     if (WAVES == 1 && J.classes <= SCORE_TILE && __ballot(a.s < SURE)) {   // (from the cache, and from its first class on wherever that
       constexpr int V = Element<TYPE>::V;                                  // lies: a lane has the same 16 of equal rows)
       // (which lanes have which places would be worked out in front of the loop over rows, and kept: 100000 rows of 1000 bf16, 16 best,
@@ -630,7 +631,7 @@ __global__ void __launch_bounds__(ST) k_scores_join(ScoreJob J) {
       for (int o = 1; o < ST / 64; ++o) list = best_of<0>(list, lds_best[o][63 - lane]);
     }
     if (J.n_top) list = with_masked<TYPE>(J, row, list);
-    give_row(J, row, lane, a, a.s - 1.0f, label, list);
+    give_row(J, row, lane, a, rest_of(a), label, list);
   }
 }
 
