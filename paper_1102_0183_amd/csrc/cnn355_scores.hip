@@ -175,7 +175,7 @@ __device__ __forceinline__ void join_lanes(Sums& a) {
 // (for all rows, 100000 of 1000 bf16 classes took 84 us, so 67; longer rows have more others).  The result: s - 1.
 constexpr float SURE = 1.5f;
 // the rest of a row that `scan` has summed: the largest value's own term is a product of two powers of two there, which may round to
-// less than 1 (in row_of, where the other kernels' rows have it too, 100000 rows of 1000 bf16 classes took 1 % longer)
+// less than 1 (in row_of, where the other kernels' rows have it too, 100000 rows of 1000 bf16 classes, read from the caches, took 1 % longer)
 __device__ __forceinline__ float rest_of(const Sums& a) { return a.s == 0.0f ? -1.0f : fmaxf(a.s - 1.0f, 0.0f); }
 template <int LANES, int N>
 __device__ __forceinline__ float rest_of(const Sums& a, const float (&x)[N]) {
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(threads_of(WAVES)) k_scores(ScoreJob J) {
     if (WAVES == 1 && J.classes <= SCORE_TILE && __ballot(a.s < SURE)) {   // (from the cache, and from its first class on wherever that
       constexpr int V = Element<TYPE>::V;                                  // lies: a lane has the same 16 of equal rows)
       // (which lanes have which places would be worked out in front of the loop over rows, and kept: 100000 rows of 1000 bf16, 16 best,
-      // took 193 us so, 187 like this)
+      // read from the caches, took 193 us so, 187 like this)
       int end = J.classes;
       asm volatile("" : "+s"(end));
       v4u r[16 / V];
