@@ -433,10 +433,10 @@ int cnn_deform_images(void* hip_stream, const float* d_src, size_t n_src, float*
  *     free for other use once the stream has passed the call; calls that may overlap need one each.
  *   cnn_class_scores_grad: d_grad, rows of `classes` elements of `type`, grad_stride apart, receives
  *     g_l[row] d log p_label / dx + g_H[row] dH / dx, that is g_l ([j == label] - p_j) - g_H p_j (log p_j + H),
- *     rounded once.  d_g_log_probs or d_g_entropy (NULL: zero) are [rows]; d_labels goes with the first, d_entropy
- *     (from cnn_class_scores) with the second.  d_grad may be d_logits with the same stride; otherwise what lies
- *     between the first and the last element of one must not overlap the other.  What lies between the rows is
- *     left as it is.  (The error -log p_label averaged over n rows: g_l = -1/n.)
+ *     rounded once (p_j below 2^-126 counts as 0 in it).  d_g_log_probs or d_g_entropy (NULL: zero) are [rows];
+ *     d_labels goes with the first, d_entropy (from cnn_class_scores) with the second.  d_grad may be d_logits with
+ *     the same stride; otherwise what lies between the first and the last element of one must not overlap the other.
+ *     What lies between the rows is left as it is.  (The error -log p_label averaged over n rows: g_l = -1/n.)
  * Sums are fp32 for every type; the same call gives the same bits, and its last ones may depend on how many rows there are and
  * which outputs are asked for.  hip_stream: a hipStream_t (NULL: the default stream) of the current device.
  * Asynchronous; nothing is allocated.  rows up to 2^31 - 1, classes up to 2^30; rows == 0 does nothing.

@@ -743,7 +743,7 @@ __device__ __forceinline__ GradRow grad_row(const ScoreGradJob& J, long long row
   r.a = J.g_entropy ? r.b * J.entropy[row] : 0.0f;
   return r;
 }
-// of one class; a class of probability zero has none but its label's
+// of one class; a class of probability zero has none but its label's (so has one below 2^-126: the exponential gives no subnormal numbers)
 __device__ __forceinline__ float grad_of(const GradRow& r, float with_label, float x) {   // (with_label: a + g_label)
   const float log_p = (x - r.m) - r.log_s, p = __builtin_amdgcn_exp2f(log_p * LOG2E);
   const float g = p == 0.0f ? 0.0f : -p * fmaf(r.b, log_p, with_label);
