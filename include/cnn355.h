@@ -229,7 +229,9 @@ int cnn_train_many(cnn_t* net, const float* d_images, const int32_t* d_labels, s
  * hold an infinity or NaN leave the weights as they are).  d_norms: [n] receives N of every image, rounded as there (0 where it
  * was skipped for its label), or NULL.  Every image's gradients go through memory, so the weights cannot stay on the chip
  * between images: one launch an image more than cnn_train_step up to 122880 weights, two from there on.  max_norm >= 0, lr
- * finite (CNN_E_ARG).  Asynchronous. */
+ * finite (CNN_E_ARG).  Asynchronous.  May be captured into a HIP graph in CNN_MODE_STAGES; in the other modes, whose launches
+ * are cooperative and (CNN_MODE_RESIDENT) carry the numbers of their images, a stream that is being captured is refused
+ * (CNN_E_STATE). */
 int cnn_train_many_clipped(cnn_t* net, const float* d_images, const int32_t* d_labels, size_t n, float lr,
                            float max_norm, float* d_norms);
 

@@ -3130,6 +3130,11 @@ int cnn_score_batch(cnn_t* net, const float* d_images, size_t n, const int32_t* 
 int cnn_train_many_clipped(cnn_t* net, const float* d_images, const int32_t* d_labels, size_t n, float lr, float max_norm, float* d_norms) {
   if (!net || !d_images || !d_labels) return fail(net ? &net->err : nullptr, CNN_E_ARG, "NULL argument");
   if (!(max_norm >= 0.f) || !std::isfinite(lr)) return fail(&net->err, CNN_E_ARG, "cnn_train_many_clipped: max_norm is negative or NaN, or lr not finite");
+  // (the resident kernel knows its images' values by numbers in its arguments: a replay's are those of values that are there already,
+  // and the grid of either needs its launch to be a cooperative one)
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (net->mode != CNN_MODE_STAGES && hipStreamIsCapturing(net->stream, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)
+    return fail(&net->err, CNN_E_STATE, "cnn_train_many_clipped: the stream is being captured, which only CNN_MODE_STAGES allows");
   // all weights, and all gradients, are one tensor
   TensorJob J;
   J.table = nullptr; J.tensors = 1; J.classes = net->n_classes;

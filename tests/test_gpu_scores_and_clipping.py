@@ -390,3 +390,48 @@ def test_clipped_steps_of_a_large_net(name, mode):
             assert (np.abs(g.get_weights() - want) <= np.abs(want) * U + step * np.abs(grad) * U * 1e-3).all()
     for net in (g, r):
         net.close()
+
+
+def test_captured_clipped_steps():
+    """Recorded in stage mode, and replayed on labels and weights as they are then; refused in the modes whose launches are cooperative,
+    before anything is launched."""
+    import torch
+    wl = synth.WORKLOADS["cfg1"]
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        r, _ = build_pair(wl)
+    g, _ = build_pair(wl)
+    for net in (g, r):
+        net.set_mode(binding.MODE_STAGES)
+    n = 3
+    d_imgs, d_labs = to_dev(synth.images(wl, n)), to_dev(synth.labels(wl, n))
+    norms, want = torch.zeros(n, device="cuda:0"), torch.zeros(n, device="cuda:0")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        r.train_many_clipped(d_imgs, d_labs, 0.05, 0.3, norms)
+    for _ in range(4):
+        graph.replay()
+        g.train_many_clipped(d_imgs, d_labs, 0.05, 0.3, want)
+        torch.cuda.synchronize()
+        assert torch.equal(norms, want) and (norms > 0).all()
+        np.testing.assert_array_equal(r.get_weights(), g.get_weights())
+        d_labs.copy_((d_labs + 1) % wl.n_classes)
+        torch.cuda.synchronize()
+    before = r.get_weights()
+    some = torch.zeros(1, device="cuda:0")
+    for mode in (binding.MODE_PERSISTENT, binding.MODE_RESIDENT):
+        r.set_mode(mode)
+        r.synchronize()
+        with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=s):
+            with pytest.raises(binding.CnnError) as e:
+                r.train_many_clipped(d_imgs, d_labs, 0.05, 0.3, norms)
+            some.add_(1)       # (a graph of something)
+        assert e.value.code == binding.E_STATE
+        np.testing.assert_array_equal(r.get_weights(), before)
+        r.train_many_clipped(d_imgs, d_labs, 0.05, 0.3, norms)      # the handle goes on
+        r.synchronize()
+        assert (norms > 0).all()
+        before = r.get_weights()
+    for net in (g, r):
+        net.close()
