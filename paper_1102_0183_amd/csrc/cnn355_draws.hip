@@ -245,11 +245,11 @@ __global__ __launch_bounds__(256) void k_draw_wave(DrawJob J) {
       if (v[j] > -__builtin_inff()) least = fminf(least, v[j]);
     }
     most = most_over(most);
-    if (s.bad || __ballot(bad) || !(__builtin_fabsf(most) < __builtin_inff())) {
+    const bool none = s.bad || __ballot(bad) != 0;   // (here, where all lanes are asked)
+    if (none || !(__builtin_fabsf(most) < __builtin_inff())) {
       if (lane == 0) {
-        const bool empty = !s.bad && !__ballot(bad) && most < 0.f;
         J.drawn[row] = -1;
-        if (J.log_probs) J.log_probs[row] = empty ? -__builtin_inff() : __builtin_nanf("");
+        if (J.log_probs) J.log_probs[row] = !none && most < 0.f ? -__builtin_inff() : __builtin_nanf("");
       }
       continue;
     }
