@@ -899,6 +899,7 @@ __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
         return v;
       };
       lowest = least_of_all(lowest);
+      cut = lowest - 1;   // (no border: all of the list stay, and nothing below it, where top-k asked for just as many)
       double left_mass = top_mass;
       int same = 0;
       for (int step = 0; step < 2; ++step) {   // top-k, top-p

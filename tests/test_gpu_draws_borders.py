@@ -4,7 +4,7 @@ import math
 
 import pytest
 
-from tests.test_gpu_draws import TYPES, _call
+from tests.test_gpu_draws import TYPES, _call, _check
 
 pytestmark = pytest.mark.gpu
 
@@ -22,3 +22,20 @@ def test_a_nan_in_any_class_of_a_row_below_zero(n, dtype):
         out, lp = _call(x, torch.full((len(places) + 1,), 0.5, device="cuda:0"))
         assert (out[:-1] == -1).all() and torch.isnan(lp[:-1]).all(), (n, rest, places, lp.tolist())
         assert (lp[-1].item() == -math.inf) == (rest == -math.inf) and not math.isnan(lp[-1].item())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,k,block", [(1500, 180, 8), (4000, 300, 8), (16000, 900, 16), (20000, 700, 16), (20000, 1100, 16), (50001, 700, 32), (50001, 1000, 32)])
+def test_as_many_classes_from_a_value_on_as_top_k_asks_for(n, k, block, dtype):
+    """k classes above the others, one in a block of neighbours each, its last: the list of candidates is what is left, and the block's others are
+    not.  With one class more or less asked for, and with a min-p that leaves all of them."""
+    import torch
+    rows = 24
+    x = torch.full((rows, n), 9.5, device="cuda:0")
+    high = torch.arange(k, device="cuda:0") * block + block - 1
+    x[:, high] = 10.0
+    x[rows // 2:, high] += torch.arange(k, device="cuda:0") % 7 * 0.0625   # (the same in all three types)
+    x = x.to(getattr(torch, dtype))
+    u = (torch.arange(rows, device="cuda:0").float() + 0.37) / rows
+    for s in ({"k": [k] * rows}, {"k": [k + 1 - r % 3 for r in range(rows)]}, {"k": [k] * rows, "q": [0.1] * rows}, {"k": [k] * rows, "p": [0.5 + 0.02 * r for r in range(rows)]}):
+        _check(x, u, **s)
