@@ -238,3 +238,25 @@ def test_a_layer_of_the_library_in_4_bits(scale_type, dtype, kind):
     # a weight is off by half a step (1 of 7, or a part of 6 between 4 and 6) and the rounding of its scale
     step = (0.5 if kind == CODES_INT4 else 1.0) / (7 if kind == CODES_INT4 else 6) + 2.0 ** -7
     assert (held.cpu().numpy() - w).__abs__().max() <= 0.05 * step
+
+
+@pytest.mark.parametrize("kind,codes_of", [(CODES_INT4, (9, 7)), (CODES_E2M1, (2, 10))])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 20, 5), (3, 32, 5), (2, 64, 40), (20, 200, 40), (40, 224, 3000), (66, 160, 12345), (66, 33, 24600)])
+def test_an_infinite_scale_makes_its_output_infinite(rows, n_in, n_out, group, dtype, kind, codes_of):
+    """The last group's, whose columns end inside a slab: y is infinite with the sign of the group's sum, not NaN, and other outputs are as they were."""
+    import math
+    import torch
+    x = torch.ones(rows, n_in, device="cuda:0", dtype=getattr(torch, dtype))
+    codes = torch.full((n_out, (n_in + 1) // 2), codes_of[0] * 17, dtype=torch.uint8, device="cuda:0")
+    codes[3] = codes_of[1] * 17   # values of -1
+    scales = torch.full((n_out, -(-n_in // group)), 0.5, device="cuda:0", dtype=x.dtype)
+    clean = _run(x, codes, scales, group, kind)
+    scales[1, -1] = scales[3, -1] = math.inf
+    scales[n_out - 1, -1] = -math.inf
+    y = _run(x, codes, scales, group, kind)
+    for o, want in ((1, math.inf), (3, -math.inf), (n_out - 1, -math.inf)):
+        assert (y[:, o] == want).all(), (o, y[:, o])
+    y[:, 1], y[:, 3], y[:, n_out - 1] = clean[:, 1], clean[:, 3], clean[:, n_out - 1]
+    assert torch.equal(y, clean) and torch.isfinite(clean).all()
