@@ -1219,7 +1219,11 @@ __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
         first_part = p1 + 1;
         continue;
       }
-      if (n == 0) break;
+      if (n == 0) {   // the sums of two passes lie on either side of the border, by their rounding: what is above the empty list stays, and no more
+        cut = over_from - 1;
+        ties = 0;
+        break;
+      }
       if (first_rank == last_rank) {   // all of the list have the same value (block_ties has their numbers)
         cut = first_rank;
         tie_weight = weight_of((double)of_rank<TYPE>(cut) - m, s, S.table);

@@ -2,6 +2,7 @@
 bits of test_gpu_draws, and its tolerances.  Needs a GPU."""
 import math
 
+import numpy as np
 import pytest
 
 from tests.test_gpu_draws import TYPES, _call, _check
@@ -39,3 +40,59 @@ def test_as_many_classes_from_a_value_on_as_top_k_asks_for(n, k, block, dtype):
     u = (torch.arange(rows, device="cuda:0").float() + 0.37) / rows
     for s in ({"k": [k] * rows}, {"k": [k + 1 - r % 3 for r in range(rows)]}, {"k": [k] * rows, "q": [0.1] * rows}, {"k": [k] * rows, "p": [0.5 + 0.02 * r for r in range(rows)]}):
         _check(x, u, **s)
+
+
+def _weights(x):
+    """exp(x) for x <= 0 as the kernels sum it up: a power of two out of 256 and three terms of the series, each rounded to 64 bits."""
+    L, t = math.log(2.0) / 256, np.maximum(np.asarray(x, np.float64), -900.0)
+    z = t.astype(np.longdouble) * np.longdouble(256.0 * 1.4426950408889634074)
+    k = np.rint(z)
+    f, series = z - k, np.full(t.shape, L ** 3 / 6)
+    for term in (L * L / 2, L, 1.0):
+        series = (series.astype(np.longdouble) * f + np.longdouble(term)).astype(np.float64)
+    k = k.astype(np.int64)
+    return (t >= -700) * np.ldexp(np.exp2((k & 255) / 256.0), k >> 8) * series
+
+
+def _next_to_a_border(x, left, spare, rows, step):
+    """(rows of x with two classes, `spare`, changed, p): p times the mass of a row is the mass of its `left` largest, but for so many `step`s."""
+    w = _weights(x)
+    w[list(spare)] = 0.0
+    prefix, rest = math.fsum(np.sort(w)[::-1][:left]), math.fsum(w)
+    p = np.float32(prefix / (rest + 3e-5))
+    while prefix / float(p) <= rest:
+        p = np.nextafter(p, np.float32(0))
+    out = np.repeat(x[None], rows, 0)
+    for i in range(rows):
+        want = (prefix + (i - rows // 2) * step) / float(p) - rest
+        a = np.float32(math.log(want))
+        while _weights([a])[0] >= want:
+            a = np.nextafter(a, np.float32(-np.inf))
+        out[i, spare[0]], out[i, spare[1]] = a, np.float32(math.log(want - _weights([a])[0]))
+    return out, float(p)
+
+
+@pytest.mark.parametrize("many,seed", [(410, 2), (410, 10), (500, 5), (500, 7), (900, 0), (900, 1), (900, 3), (900, 10)])
+def test_a_border_within_rounding_between_two_lists_of_a_flat_row(many, seed):
+    """Top-p of p times the mass of exactly the 9500 largest of 20000 classes, to a rounding: hundreds of classes close above the border and hundreds
+    close below, with a gap between them, so that the kernel looks at the two sides one after the other and its sums may contradict each other.
+    Drawn is one of the 9500, or of one class more (a border within rounding may fall on either side)."""
+    import torch
+    rows, draws, n, left = 16, 32, 20000, 9500
+    g = np.random.default_rng(seed)
+    above, below = -(19 + 63.5 * 3 / 128) / 16 + np.linspace(-4e-4, 4e-4, many), -(19 + 66.5 * 3 / 128) / 16 + np.linspace(-4e-4, 4e-4, 390)
+    rest = np.concatenate([[0.0], g.uniform(-1.2, 0, left - many - 1), above, below, g.uniform(-2, -1.4, n - 16 - left - 390)]).astype(np.float32)
+    x = np.concatenate([np.full(16, -2.0, np.float32), g.permutation(rest)])
+    spare = [i for i in np.argsort(x) if i >= 16][:2]
+    x, p = _next_to_a_border(x, left, spare, rows, np.spacing(5000.0))
+    x = torch.from_numpy(x).to("cuda:0").repeat_interleave(draws, 0)
+    u = torch.from_numpy(g.random(rows * draws).astype(np.float32)).to("cuda:0")
+    out, lp = _call(x, u, p=[p] * (rows * draws))
+    border = torch.sort(x[0], descending=True)[0][left]
+    drawn = x.gather(1, out.long()[:, None])[:, 0]
+    # the log probability of it among the 9500, or the 9501: 5e-5 apart
+    w = torch.sort(x.double().exp(), 1, descending=True)[0]
+    mass = w[:, :left].sum(1)
+    off = torch.stack([lp.double() - (drawn.double() - m.log()) for m in (mass, mass + w[:, left])]).abs().min(0)[0]
+    assert (off <= 2.0 ** -24 * lp.double().abs() + 1e-12).all()
+    assert (drawn >= border).all(), (torch.nonzero(drawn < border)[:, 0] // draws, drawn[drawn < border], border)
