@@ -84,6 +84,12 @@ __device__ __forceinline__ void fill_table(double* table, int threads) {
 __device__ __forceinline__ double weight_of(double t, const Settings& s, const double* table) {
   return t < s.low ? 0.0 : exp_of(t, s.c, table);
 }
+// A w in units of 2^-51, 1 at least if it is not 0: sums of up to 2048 of them, in any order, are off by 4.5e-13 at most.
+constexpr double UNIT = 0x1p-51;
+__device__ __forceinline__ u64 units_of(double w) {
+  const u64 units = __builtin_bit_cast(u64, __builtin_fma(w, 1 / UNIT, 0x1p52)) & 0xfffffffffffffull;
+  return w > 0.0 && !units ? 1 : units;
+}
 
 // ---- between lanes ----
 template <int D>
@@ -91,6 +97,8 @@ __device__ __forceinline__ double xor_lane(double v) {
   const u64 b = __builtin_bit_cast(u64, v);
   return __builtin_bit_cast(double, (u64)xor_word<D>((unsigned)(b >> 32)) << 32 | xor_word<D>((unsigned)b));
 }
+template <int D>
+__device__ __forceinline__ u64 xor_lane(u64 v) { return (u64)xor_word<D>((unsigned)(v >> 32)) << 32 | xor_word<D>((unsigned)v); }
 template <int D>
 __device__ __forceinline__ float xor_lane(float v) { return __builtin_bit_cast(float, xor_word<D>(__builtin_bit_cast(unsigned, v))); }
 template <int D>
@@ -386,7 +394,7 @@ struct Shared {
   double wave_sum[THREADS / 64];
   int wave_count[THREADS / 64];
   int wave_ranks[THREADS / 64][2], pair_count[2][THREADS / 64];
-  double pair_mass[2][THREADS / 64];
+  u64 pair_mass[2][THREADS / 64];
   float wave_most[THREADS / 64], wave_least[THREADS / 64];
   double before, aim;
   int chosen, last, listed, blocks;
@@ -874,11 +882,11 @@ __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
     }
     if (n > THREADS && n <= MOST) {
       // More of them than are sorted quickly: borders by halves, a count or a mass of the list's classes from a bound on at a time, and masses
-      // block by block, as whole numbers, whose order does not matter (37 rows of 50001 with top-p 0.9, mostly such lists, 53 us with two bitonic
+      // block by block, all as whole numbers: which class comes to which thread is the wavefronts' race, and does not matter to their sums (37 rows of 50001 with top-p 0.9, mostly such lists, 53 us with two bitonic
       // sorts, so 42; 2000 of 4000 102 and 90).
       constexpr int EACH = MOST / THREADS;
       int ranks[EACH], index[EACH], lowest = 0x7fffffff;
-      double w[EACH];
+      u64 w[EACH];
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         const bool in = tid + i * THREADS < n;
@@ -886,7 +894,7 @@ __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
         const float v = value_of(order_in(key));
         ranks[i] = in ? rank_of<TYPE>(v) : -0x7fffffff;   // (below all; its negative is a whole number too)
         index[i] = index_in(key);
-        w[i] = in ? weight_of((double)v - m, s, S.table) : 0.0;
+        w[i] = in ? units_of(weight_of((double)v - m, s, S.table)) : 0;
         lowest = in ? min(lowest, ranks[i]) : lowest;
       }
       auto least_of_all = [&](int v) {
@@ -905,10 +913,11 @@ __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
       for (int step = 0; step < 2; ++step) {   // top-k, top-p
         if (step == 0 ? s.k >= n : !s.by_p) continue;
         if (step == 1 && by_k && s.k >= n) {   // (all of the list are what top-k leaves)
-          double sum = 0.0;
+          u64 sum = 0;
 #pragma unroll
           for (int i = 0; i < EACH; ++i) sum += w[i];
-          sum_before<THREADS>(sum, S.wave_sum, &left_mass);
+          sum_before<THREADS>(sum, S.pair_mass[1], &sum);   // (the first halving writes the other one)
+          left_mass = (double)sum * UNIT;
         }
         const double need = s.p * left_mass;
         int low = lowest, high = rank_of<TYPE>(most) + 1, n_low = n, n_high = 0;
@@ -916,25 +925,26 @@ __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
         for (int i = 0; (unsigned)high - (unsigned)low > 1u && n_low - n_high > 1; ++i) {
           const int mid = between<TYPE>(low, high, i);
           int count = 0;
-          double mass = 0.0;
+          u64 units = 0;
 #pragma unroll
           for (int k = 0; k < EACH; ++k) {
             count += __popcll(__ballot(ranks[k] >= mid));
-            mass += ranks[k] >= mid ? w[k] : 0.0;
+            units += ranks[k] >= mid ? w[k] : 0;
           }
-          mass = sum_over(mass);
+          units = sum_over(units);
           if (lane == 0) {
             S.pair_count[i & 1][wave] = count;
-            S.pair_mass[i & 1][wave] = mass;
+            S.pair_mass[i & 1][wave] = units;
           }
           __syncthreads();
           count = 0;
-          mass = 0.0;
+          units = 0;
 #pragma unroll
           for (int k = 0; k < THREADS / 64; ++k) {
             count += S.pair_count[i & 1][k];
-            mass += S.pair_mass[i & 1][k];
+            units += S.pair_mass[i & 1][k];
           }
+          const double mass = (double)units * UNIT;
           if (step ? mass >= need : count >= s.k) {
             low = mid;
             n_low = count;
@@ -973,14 +983,11 @@ __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         if (tid + i * THREADS >= n || (s.by_min && (double)of_rank<TYPE>(ranks[i]) - m < s.bound)) continue;
-        if (ranks[i] > cut && w[i] > 0.0) {   // (in units of 2^-51, 4.5e-13 of 2048 classes at most; none is lost)
-          const u64 units = __builtin_bit_cast(u64, __builtin_fma(w[i], 0x1p51, 0x1p52)) & 0xfffffffffffffull;
-          atomicAdd(&fixed[index[i] >> block_log2], units ? units : 1);
-        }
+        if (ranks[i] > cut && w[i]) atomicAdd(&fixed[index[i] >> block_log2], w[i]);
         if (ties && ranks[i] == cut) atomicAdd(&block_ties[index[i] >> block_log2], 1);
       }
       __syncthreads();
-      for (int b = tid; b < blocks; b += THREADS) block_mass[b] = (double)fixed[b] * 0x1p-51;
+      for (int b = tid; b < blocks; b += THREADS) block_mass[b] = (double)fixed[b] * UNIT;
       masses_there = true;
     }
   }

@@ -96,3 +96,25 @@ def test_a_border_within_rounding_between_two_lists_of_a_flat_row(many, seed):
     off = torch.stack([lp.double() - (drawn.double() - m.log()) for m in (mass, mass + w[:, left])]).abs().min(0)[0]
     assert (off <= 2.0 ** -24 * lp.double().abs() + 1e-12).all()
     assert (drawn >= border).all(), (torch.nonzero(drawn < border)[:, 0] // draws, drawn[drawn < border], border)
+
+
+@pytest.mark.parametrize("n,block,live,left,k", [(9000, 8, 900, 450, 0), (9000, 8, 600, 400, 600), (20000, 16, 1200, 700, 0), (20000, 16, 700, 350, 700),
+                                                 (20000, 16, 1200, 650, 900), (50001, 32, 1500, 800, 0), (50001, 32, 900, 500, 900)])
+def test_equal_rows_draw_the_same_next_to_a_border_of_rounding(n, block, live, left, k):
+    """Lists of hundreds of classes come together in any order; their masses do not depend on it.  Rows of which top-p is to leave exactly `left`
+    classes, to a rounding, many times over in one call and in calls after each other: the same bits in all of them."""
+    import torch
+    rows, copies = 12, 20 if n > 40000 else 300
+    g = np.random.default_rng(n + live)
+    x, at = np.full(n, -np.inf, np.float32), g.permutation(n // block)[:live] * block + g.integers(0, block, live)   # (one in a block of neighbours)
+    x[at] = g.uniform(-3, 0, live)
+    x[at[0]] = 0.0
+    x, p = _next_to_a_border(x, left, at[np.argsort(x[at])[:2]], rows, np.spacing(_weights(x).sum()) / 2)
+    x = torch.from_numpy(x).to("cuda:0").repeat_interleave(copies, 0)
+    u = torch.full((rows * copies,), 0.43, device="cuda:0")
+    first = None
+    for _ in range(20):
+        out, lp = _call(x, u, p=[p] * (rows * copies), k=[k] * (rows * copies))
+        got = torch.stack([out, lp.view(torch.int32)]).view(2, rows, copies)
+        first = got[:, :, :1].clone() if first is None else first
+        assert (got == first).all(), [(got[:, r] != first[:, r]).sum().item() for r in range(rows)]
