@@ -197,7 +197,8 @@ int cnn_score_batch(cnn_t* net, const float* d_images, size_t n, const int32_t* 
 
 /* The same pass with a class drawn for every image by what the output layer says of it: cnn_draw_classes (below) of the layer's
  * sums.  d_temperature, d_top_k, d_top_p, d_min_p, each [n] or NULL; d_u [n]; d_class [n]; d_log_probs [n] or NULL.  The rest as for
- * cnn_forward_batch, its scratch included.  CNN_E_STATE with CNN_OUTPUT_TANH_SQERR, CNN_E_SHAPE beyond 2^21 classes.  Asynchronous. */
+ * cnn_forward_batch, its scratch included.  What is written must overlap nothing else in the call.  CNN_E_STATE with
+ * CNN_OUTPUT_TANH_SQERR, CNN_E_SHAPE beyond 2^21 classes.  Asynchronous. */
 int cnn_draw_batch(cnn_t* net, const float* d_images, size_t n, const float* d_temperature, const int32_t* d_top_k,
                    const float* d_top_p, const float* d_min_p, const float* d_u, int32_t* d_class, float* d_log_probs,
                    void* d_scratch, size_t scratch_bytes, size_t batch);

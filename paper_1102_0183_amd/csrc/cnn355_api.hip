@@ -2926,6 +2926,24 @@ static int check_draws(const char* call, int type, size_t rows, size_t classes, 
   return CNN_OK;
 }
 
+// why the arrays of a draw are refused, or null; [x0, x1): what the classes are drawn from
+static const char* bad_draw_arrays(size_t rows, const float* d_temperature, const int32_t* d_top_k, const float* d_top_p, const float* d_min_p,
+                                   const float* d_u, const int32_t* d_class, const float* d_log_probs, uintptr_t x0, uintptr_t x1) {
+  if (!d_u || !d_class) return "NULL argument";
+  const uintptr_t words[] = {(uintptr_t)d_temperature, (uintptr_t)d_top_k, (uintptr_t)d_top_p, (uintptr_t)d_min_p, (uintptr_t)d_u, (uintptr_t)d_class, (uintptr_t)d_log_probs};
+  for (uintptr_t w : words)
+    if (w % 4) return "misaligned argument";
+  // what is written, over the rest
+  for (int w = 5; w < 7; ++w) {
+    const uintptr_t a = words[w], b = a + 4 * rows;
+    if (!a) continue;
+    if (a < x1 && x0 < b) return "what is written overlaps what is drawn from";
+    for (int o = 0; o < 7; ++o)
+      if (o != w && words[o] && words[o] < b && a < words[o] + 4 * rows) return "what is written overlaps another argument";
+  }
+  return nullptr;
+}
+
 int cnn_draw_classes_scratch_bytes(size_t rows, size_t classes, size_t* bytes) {
   if (!bytes) return fail(nullptr, CNN_E_ARG, "cnn_draw_classes_scratch_bytes: NULL argument");
   int rc = check_draws("cnn_draw_classes_scratch_bytes", CNN_TYPE_F32, rows, classes, classes);
@@ -2943,20 +2961,9 @@ int cnn_draw_classes(void* hip_stream, const void* d_logits, int type, size_t ro
   if (rc) return rc;
   if (rows == 0) return CNN_OK;
   if (!d_logits || (uintptr_t)d_logits % element_bytes(type)) return fail(nullptr, CNN_E_ARG, "cnn_draw_classes: d_logits is NULL or misaligned");
-  if (!d_u || !d_class) return fail(nullptr, CNN_E_ARG, "cnn_draw_classes: NULL argument");
-  const uintptr_t words[] = {(uintptr_t)d_temperature, (uintptr_t)d_top_k, (uintptr_t)d_top_p, (uintptr_t)d_min_p, (uintptr_t)d_u, (uintptr_t)d_class, (uintptr_t)d_log_probs};
-  for (uintptr_t w : words)
-    if (w % 4) return fail(nullptr, CNN_E_ARG, "cnn_draw_classes: misaligned argument");
-  // what is written, over the rest
   const uintptr_t x0 = (uintptr_t)d_logits, x1 = x0 + ((rows - 1) * row_stride + classes) * element_bytes(type);
-  for (int w = 5; w < 7; ++w) {
-    const uintptr_t a = words[w], b = a + 4 * rows;
-    if (!a) continue;
-    if (a < x1 && x0 < b) return fail(nullptr, CNN_E_ARG, "cnn_draw_classes: d_class or d_log_probs overlaps d_logits");
-    for (int o = 0; o < 7; ++o)
-      if (o != w && words[o] && words[o] < b && a < words[o] + 4 * rows)
-        return fail(nullptr, CNN_E_ARG, "cnn_draw_classes: what is written overlaps another argument");
-  }
+  if (const char* why = bad_draw_arrays(rows, d_temperature, d_top_k, d_top_p, d_min_p, d_u, d_class, d_log_probs, x0, x1))
+    return fail(nullptr, CNN_E_ARG, std::string("cnn_draw_classes: ") + why);
   DrawJob J;
   J.x = (const CNN_GLOBAL void*)d_logits; J.temperature = d_temperature; J.top_k = d_top_k; J.top_p = d_top_p; J.min_p = d_min_p; J.u = d_u;
   J.drawn = d_class; J.log_probs = d_log_probs;
@@ -3414,7 +3421,10 @@ int cnn_draw_batch(cnn_t* net, const float* d_images, size_t n, const float* d_t
   if (net->out_units != CNN_OUTPUT_SOFTMAX_XENT) return fail(&net->err, CNN_E_STATE, "cnn_draw_batch: the output units are not a soft-max");
   if (net->n_classes > DRAW_CLASSES) return fail(&net->err, CNN_E_SHAPE, "cnn_draw_batch: at most 2^21 classes");
   if (n == 0) return CNN_OK;
-  if (!d_u || !d_class) return fail(&net->err, CNN_E_ARG, "cnn_draw_batch: NULL argument");
+  const uintptr_t x0 = (uintptr_t)d_images, x1 = x0 + n * net->image_size * sizeof(float), s0 = (uintptr_t)d_scratch, s1 = s0 + scratch_bytes;
+  const char* why = bad_draw_arrays(n, d_temperature, d_top_k, d_top_p, d_min_p, d_u, d_class, d_log_probs, x0, x1);
+  if (!why) why = bad_draw_arrays(n, d_temperature, d_top_k, d_top_p, d_min_p, d_u, d_class, d_log_probs, s0, s1);
+  if (why) return fail(&net->err, CNN_E_ARG, std::string("cnn_draw_batch: ") + why);
   DrawJob J;
   J.x = nullptr; J.temperature = d_temperature; J.top_k = d_top_k; J.top_p = d_top_p; J.min_p = d_min_p; J.u = d_u;
   J.drawn = d_class; J.log_probs = d_log_probs; J.part_mass = nullptr; J.part_max = nullptr;

@@ -5,6 +5,7 @@ import math
 import numpy as np
 import pytest
 
+from paper_1102_0183_amd import binding
 from tests.test_gpu_draws import TYPES, _call, _check
 
 pytestmark = pytest.mark.gpu
@@ -118,3 +119,34 @@ def test_equal_rows_draw_the_same_next_to_a_border_of_rounding(n, block, live, l
         got = torch.stack([out, lp.view(torch.int32)]).view(2, rows, copies)
         first = got[:, :, :1].clone() if first is None else first
         assert (got == first).all(), [(got[:, r] != first[:, r]).sum().item() for r in range(rows)]
+
+
+def test_arrays_that_classes_of_images_are_not_drawn_with():
+    """Misaligned arrays, and results over what the call reads, are refused as cnn_draw_classes refuses them; nothing is written."""
+    import torch
+    net = binding.Cnn("1x12x12-4C3-MP2-30N-200N")
+    rng = np.random.default_rng(1)
+    net.set_weights(rng.uniform(-0.08, 0.08, net.num_weights).astype(np.float32))
+    n = 6
+    images = torch.from_numpy(rng.uniform(-1, 1, (n, net.image_size)).astype(np.float32)).to("cuda:0")
+    scratch = torch.zeros(net.forward_batch_scratch_bytes(n), dtype=torch.uint8, device="cuda:0")
+    words = torch.zeros(7 * 64, dtype=torch.int32, device="cuda:0")
+    keep = images.clone()
+    T, k, p, q, u, out, lp = (words.data_ptr() + 256 * i for i in range(7))
+    words.view(torch.float32)[:64] = 1.0   # (T)
+
+    def call(x=images.data_ptr(), T=T, k=k, p=None, q=q, u=u, out=out, lp=lp, scratch=scratch):
+        torch.cuda.synchronize()
+        return binding.lib().cnn_draw_batch(net._h, x, n, T, k, p, q, u, out, lp, scratch.data_ptr(), scratch.numel(), n)
+    before = words.clone()
+    for kw in (dict(u=None), dict(out=None), dict(T=T + 2), dict(k=k + 1), dict(p=p + 3), dict(q=q + 2), dict(u=u + 1), dict(out=out + 2), dict(lp=lp + 2),
+               dict(out=u), dict(out=u + 4 * (n - 1)), dict(out=k - 4), dict(lp=out), dict(lp=out - 4), dict(lp=T), dict(out=images.data_ptr()),
+               dict(lp=images.data_ptr() + 4 * (images.numel() - 1)), dict(out=scratch.data_ptr()), dict(lp=scratch.data_ptr() + scratch.numel() - 4)):
+        assert call(**kw) == binding.E_ARG, kw
+        assert "cnn_draw_batch" in binding._err(net._h), kw
+    net.synchronize()
+    assert torch.equal(words, before) and torch.equal(images, keep)
+    assert call() == 0 and call(lp=None) == 0 and call(lp=out + 4 * n) == 0
+    net.synchronize()
+    assert (words.view(7, 64)[5, :n] >= 0).all()
+    net.close()
