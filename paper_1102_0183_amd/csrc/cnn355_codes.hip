@@ -307,7 +307,8 @@ __global__ __launch_bounds__((64 * WAVES<RT, OT>)) void k_product(ProductJob J) 
     ask(std::false_type(), whole, slab[0]);
     add(slab[0], [&](int o, int step) {
       const int g = (whole * PRODUCT_SLAB + step * STEPS * 32) >> J.group_log2;
-      return g < J.groups ? E::get(scales[o][g]) : 0.f;   // (past the columns: an infinite scale times none of them is nothing)
+      const float scale = E::get(scales[o][g < J.groups ? g : J.groups - 1]);
+      return g < J.groups ? scale : 0.f;   // (past the columns: an infinite scale times none of them is nothing)
     });
   }
   __syncthreads();
@@ -327,8 +328,11 @@ __global__ __launch_bounds__((64 * WAVES<RT, OT>)) void k_product(ProductJob J) 
     if (out >= J.n_out || row >= J.rows) continue;
     float v = 0.f;
 #pragma unroll
-    for (int p = 0; p < PC && !(p && __builtin_isinf(v)); ++p)   // (of an infinite scale the other pieces, zeros mostly, make NaN)
+    for (int p = 0; p < PC; ++p) {
+      const float before = v;
       for (int k = 0; k < waves; ++k) v += red[(((k * RT + r / TR) * OT + o) * 16 + r % TR * PC + p) * 16 + c];
+      if (p && __builtin_isinf(before)) v = before;   // (an infinite scale's: it makes NaN of the other pieces' sums, nothing mostly)
+    }
     if (KIND == CODES_INT4) v *= 16.f;
     if (J.bias) v += J.bias[out];
     if (J.y_type == ELEMENT_F32) ((CNN_GLOBAL float*)J.y)[row * J.y_stride + out] = v;
@@ -463,7 +467,8 @@ __global__ __launch_bounds__(TILE_THREADS) void k_product_tile(ProductJob J) {
     if (!half)
       add(0, w, [&](int o, int step) {
         const int g = (k0 + step * STEPS * 32) >> J.group_log2;
-        return g < J.groups ? E::get(scales[o][g]) : 0.f;
+        const float scale = E::get(scales[o][g < J.groups ? g : J.groups - 1]);
+        return g < J.groups ? scale : 0.f;
       });
   }
   __syncthreads();
@@ -493,7 +498,11 @@ __global__ __launch_bounds__(TILE_THREADS) void k_product_tile(ProductJob J) {
     if (out >= J.n_out || row >= J.rows) continue;
     float v = 0.f;
 #pragma unroll
-    for (int p = 0; p < PC && !(p && __builtin_isinf(v)); ++p) v += red[(r / TR * 16 + r % TR * PC + p) * TILE_OUTS + o];
+    for (int p = 0; p < PC; ++p) {
+      const float before = v;
+      v += red[(r / TR * 16 + r % TR * PC + p) * TILE_OUTS + o];
+      if (p && __builtin_isinf(before)) v = before;   // (an infinite scale's)
+    }
     if (KIND == CODES_INT4) v *= 16.f;
     if (J.bias) v += J.bias[out];
     if (J.y_type == ELEMENT_F32) ((CNN_GLOBAL float*)J.y)[row * J.y_stride + out] = v;
