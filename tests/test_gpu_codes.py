@@ -260,3 +260,46 @@ def test_an_infinite_scale_makes_its_output_infinite(rows, n_in, n_out, group, d
         assert (y[:, o] == want).all(), (o, y[:, o])
     y[:, 1], y[:, 3], y[:, n_out - 1] = clean[:, 1], clean[:, 3], clean[:, n_out - 1]
     assert torch.equal(y, clean) and torch.isfinite(clean).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_in,n_out", [(3, 700, 90), (16, 300, 50), (40, 1000, 70), (30, 260, 10000), (66, 523, 12345)])
+def test_a_row_does_not_depend_on_the_others(rows, n_in, n_out, dtype):
+    """As many rows, but others beside it (numbers, infinities, NaN): the same bits, first, last and between tiles."""
+    import math
+    import torch
+    codes, scales, _ = _layer(n_out, n_in, 64, dtype, CODES_INT4, 2)
+    a, b = _rows(rows, n_in, dtype, 1), _rows(rows, n_in, dtype, 2)
+    keep = sorted({0, 2, rows // 2, rows - 1})
+    b[1], b[rows - 2, ::3] = math.nan, math.inf
+    b[keep] = a[keep]
+    y, z = (_run(x, codes, scales, 64, CODES_INT4, None, torch.float32) for x in (a, b))
+    assert torch.isfinite(y).all() and torch.equal(y[keep], z[keep])
+    others = [r for r in range(rows) if r not in keep]
+    assert (y[others] != z[others]).any(1).all()
+
+
+def test_small_numbers_of_32_bits():
+    """What bits a float has of 2^-133 and above count, all of them; those below count as 0."""
+    import torch
+    n_in, rows = 64, 150
+    gen = torch.Generator(device="cuda:0").manual_seed(5)
+    x = torch.zeros(rows, n_in, dtype=torch.float64, device="cuda:0")
+    x[:, 0] = (1 + torch.rand(rows, generator=gen, device="cuda:0", dtype=torch.float64)) * torch.exp2(-torch.arange(rows, device="cuda:0").double())
+    x[1::2] *= -1
+    x = x.float()
+    codes = torch.full((16, n_in // 2), 0x88, dtype=torch.uint8, device="cuda:0")
+    scale = 2.0 ** 100
+    scales = torch.full((16, 2), scale, device="cuda:0")
+    for kind in (CODES_INT4, CODES_E2M1):
+        codes.fill_(0x88 if kind == CODES_INT4 else 0)
+        codes[:, 0] += torch.arange(16, device="cuda:0", dtype=torch.uint8) - (8 if kind == CODES_INT4 else 0)
+        y = _run(x, codes, scales, 32, kind)
+        values = torch.tensor(VALUES[kind], dtype=torch.float64, device="cuda:0")
+        v = x[:, 0].double()
+        want = v[:, None] * values * scale
+        held = torch.trunc(v * 2.0 ** 133) * 2.0 ** -133
+        # three pieces of 8 bits, cut off: exact where the last one ends at 2^-133 or above; products and their sum are rounded three times
+        assert ((y.double() - held[:, None] * values * scale).abs() <= 3 * U * want.abs()).all()
+        whole = v.abs() >= 2.0 ** -109
+        assert ((y.double() - want).abs() <= 3 * U * want.abs())[whole].all()

@@ -295,3 +295,26 @@ def test_rows_beyond_32_bits():
     _check(out, x, None, None, 0.5, 1, 2, "bfloat16")
     binding.dropout(out, x, 0.0, 1, 2)
     assert torch.equal(x, out)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(200, 515), (31, 4000)])
+def test_the_largest_share_below_all_of_them(rows, cols, dtype):
+    """p = 1 - 2^-24: 256 numbers of 2^32 keep a unit, times 2^24.  Steps whose masks keep one, some or none, found by the definition."""
+    import torch
+    p, seed = 1.0 - 2.0 ** -24, 77
+    gen = torch.Generator(device="cuda:0").manual_seed(rows)
+    x, residual, bias = (_matrix(n, cols, dtype, gen, scale=2.0 ** -14) for n in (rows, rows, 1))
+    bias = bias[0].contiguous()
+    kept = [int(_kept(rows, cols, p, seed, step).sum()) for step in range(400)]
+    some = [s for s in range(400) if kept[s]]
+    assert some and _factor(p) == 2.0 ** 24
+    out, g_bias = torch.empty_like(x), torch.empty(cols, device=x.device)
+    for step in some[:3] + [kept.index(0)]:
+        binding.dropout(x, out, p, seed, step)
+        _check(out, x, None, None, p, seed, step, dtype)
+        binding.dropout(x, out, p, seed, step, bias, residual)
+        _check(out, x, bias, residual, p, seed, step, dtype)
+        binding.dropout_grad(x, out, p, seed, step, g_bias, _scratch(rows, cols))
+        _check_grad(out, g_bias, x, p, seed, step, dtype)
+        assert int((out != 0).sum()) == kept[step]
