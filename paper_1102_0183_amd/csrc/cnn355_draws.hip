@@ -589,9 +589,10 @@ __device__ __forceinline__ void sort_keys(u64* key, int n) {
 }
 
 // A workgroup a row.  PARTS: other workgroups have looked at it.  MANY: the rows of whose classes the first kernel finds many left (and
-// marks so): the code that settles those takes the registers of another workgroup (some 200; the first kernel has
-// 86).  Neither spills any, and neither is to: bounded so that it did, one kernel for both gave wrong rows.  Without a marked row this launch
-// takes 4 us.
+// marks so): the code that settles those takes the registers of another workgroup (some 200 vector registers; the first
+// kernel has 86, or 111 with 256 threads).  No vector register is spilled (scalar ones go to lanes of vector registers: 59 to 76 in the second), and
+// none is to be: bounded so that some were, one kernel for both gave wrong rows, which a second reading of its source did not explain either; a
+// test holds the compiler to it.  Without a marked row this launch takes 4 us.
 constexpr int MARK = -2;
 template <int TYPE, int THREADS, int MOST, bool PARTS, bool MANY>
 __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
@@ -735,9 +736,8 @@ __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
   bool masses_there = false;   // of what stays, block by block
   if (!MANY && !all_count) {
     constexpr int PER = DRAW_BLOCKS / THREADS;
-    const bool all = classes <= MOST && !(by_k && s.k <= blocks);
     int from = rank_of<TYPE>(-3.4028234663852886e38f), n_from = -1, held = 0;   // (held: blocks that are not switched off)
-    if ((by_k || s.by_p) && !all) {
+    if (by_k || s.by_p) {
       int ranks[PER];
       u64 weights[PER];
       const u64 need = (u64)(s.p * top_mass * 0x1p40) + 1;
@@ -825,7 +825,7 @@ __global__ __launch_bounds__(THREADS) void k_draw(DrawJob J) {
     const bool by_rank = n_from >= 0;
     // (a list that will not do costs a second look: where b of B blocks of many classes hold some, about -B ln(1 - b / B) classes are meant)
     const int limit = classes <= 2 * MOST ? blocks : (int)(blocks * (1.f - expf(-(float)MOST / blocks)));
-    const int n = all || (by_rank && n_from <= MOST) || by_bound || (by_k && !by_rank && held << block_log2 <= 4 * MOST)
+    const int n = (by_rank && n_from <= MOST) || by_bound || (by_k && !by_rank && held << block_log2 <= 4 * MOST)
                       ? list_of(limit, [&](float v) { return rank_of<TYPE>(v) >= from && !(by_bound && rank_of<TYPE>(v) < rank_of<TYPE>(bound) - 1); },
                                 [&](float v) { return rank_of<TYPE>(v) >= from && !(by_bound && (double)v - m < s.bound); })
                       : MOST + 1;
