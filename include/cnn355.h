@@ -509,7 +509,8 @@ int cnn_clipped_update(void* hip_stream, const cnn_tensor* host_weights, const c
  *   d_class [rows]; d_log_probs [rows] or NULL.
  *   d_scratch: device memory, 256-byte aligned, of at least cnn_draw_classes_scratch_bytes (host-only; 0 where rows are short or fill
  *   the chip: NULL will do), free for other use once the stream has passed the call; calls that may overlap need one each.
- * w and its sums are double, in an order that depends on the call's sizes alone: the same call gives the same classes.
+ * w and its sums are double, in an order that depends on the call's sizes alone, or whole numbers of 2^-51, in any order: the same call gives
+ * the same classes.
  * hip_stream: a hipStream_t (NULL: the default stream) of the current device.  Asynchronous; nothing is allocated.  rows up to
  * 2^31 - 1, classes up to 2^21; rows == 0 does nothing.  What is written must overlap nothing else in the call.
  * Errors: CNN_E_ARG, CNN_E_SHAPE, CNN_E_WORKSPACE, CNN_E_HIP; the message is cnn_last_error(NULL)'s. */
@@ -558,8 +559,8 @@ int cnn_dropout_grad(void* hip_stream, const void* d_g, int type, size_t rows, s
  *     that is 0 or not finite has codes of 0.  host_scales receives elements of `type`.  The unused half of a row's last byte is 0.
  *   cnn_quantised_product: y[row][o] = bias[o] + sum_i x[row][i] w[o][i] for rows of n_in elements of `type`, from one row to many;
  *     d_bias: device, fp32 [n_out], or NULL.  y is of y_type, `type` or CNN_TYPE_F32, rounded once.  x and the codes' values are
- *     multiplied exactly; the sums over 32 columns or a group, the scales' products and their sum are fp32.  What lies between the rows
- *     is left as it is; columns beyond n_in are not read.  d_y must overlap nothing else in the call.
+ *     multiplied exactly (of fp32 rows, bits below 2^-133 count as 0); the sums over 32 columns or a group, the scales' products and their
+ *     sum are fp32.  What lies between the rows is left as it is; columns beyond n_in are not read.  d_y must overlap nothing else in the call.
  * hip_stream as above.  Asynchronous; nothing is allocated.  n_in and n_out up to 2^24, rows up to 2^31 - 1; rows == 0 does nothing.
  * Errors: CNN_E_ARG, CNN_E_SHAPE, CNN_E_HIP; the message is cnn_last_error(NULL)'s. */
 enum { CNN_CODES_INT4 = 0, CNN_CODES_E2M1 = 1 };

@@ -3,7 +3,7 @@
 // what is left the class is drawn at which the sum of w, in the order of the indices, first is above u times the whole.
 //
 // A class comes out right only if sums at borders do: among 131072 classes borders lie 1e-5 of the whole apart and closer, so w
-// and its sums are double (an error of 1e-7 would draw another class every hundred rows).  An exponential is a table of 256
+// and its sums are double, or whole numbers of 2^-51 where their order is not fixed (an error of 1e-7 would draw another class every hundred rows).  An exponential is a table of 256
 // powers of two in LDS and a polynomial of three terms, off by 1.4e-13 at most: 10 operations in double, at the rate of those in
 // float.
 //
